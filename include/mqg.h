@@ -48,7 +48,7 @@ typedef enum {
     MQG_ERR_UNSUPPORTED = -4             /* valid request outside the built limits       */
 } mqg_status;
 
-typedef enum { MQG_F32 = 0, MQG_F16 = 1 } mqg_dtype;
+typedef enum { MQG_F32 = 0, MQG_F16 = 1, MQG_BF16 = 2 } mqg_dtype;   /* MQG_BF16: the calls of a layer only */
 typedef enum { MQG_I32 = 0, MQG_I64 = 1 } mqg_itype;
 
 #define MQG_MAX_FANOUT 64                /* per-node neighbour budget of one block       */
@@ -631,6 +631,115 @@ int mqg_weighted_aggregate_backward(mqg_ctx *ctx, const mqg_block *block, const 
                                     const float *self_w, const void *grad_out, int64_t go_stride,
                                     void *grad_x, int64_t gx_stride, int32_t dim, int32_t dtype,
                                     mqg_stream stream);
+
+/*
+ * ---- The calls of a layer ------------------------------------------------------------------
+ * What a training program does between two aggregations (the dense layer of Eq. 16's GraphSAGE
+ * and its products are the caller's): the norm of the hidden rows with the residual's addition, the
+ * aggregation of rows that are held in 8 bits, and the step of the weight matrices.  They take a
+ * context for errors, profiling and scratch only; its graph is not used.  Rows and matrices may
+ * be MQG_F32, MQG_F16 or MQG_BF16; strides are in elements, pointers need the alignment of an
+ * element only, and, unlike in the calls above, nothing outside a row's dim columns is read or
+ * written.  mqg_ctx_reserve_layer allocates now what mqg_rms_norm_backward (for rows of up to norm_dim
+ * columns) and mqg_orthogonalize and mqg_muon_step (for stacks of num_mats matrices of rows x cols) would
+ * otherwise allocate when they are first called at that size, after a synchronisation of the stream:
+ * 4 KiB per column; 12 bytes per element and 8 per element of the smaller side's square, sides rounded up to multiples of 128.
+ * While a stream is recorded into a HIP graph nothing is allocated: a call that would have to is
+ * refused with MQG_ERR_UNSUPPORTED.  Pass 0 for what is not wanted.
+ */
+int mqg_ctx_reserve_layer(mqg_ctx *ctx, int32_t norm_dim, int32_t num_mats, int32_t rows, int32_t cols);
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition:
+ *   s = x + residual,  y = s * 1/sqrt(mean over the columns of s^2 + eps) * weight
+ * computed in fp32 from the inputs; each output is rounded once.
+ *   residual   may be NULL: s = x
+ *   weight     device float [dim]; NULL = ones
+ *   num_rows_dev  device int64, the number of rows (e.g. &blocks[l].sizes[1]); values above cap_rows
+ *              are clamped to it, NULL = cap_rows
+ *   sum        receives s (dtype), NULL if not wanted.  What the backward takes
+ *   y          receives y (dtype), NULL if not wanted
+ *   q, scale   receive y in 8 bits, NULL if not wanted (one of y and q is): one scale per row (group = 0) or per `group`
+ *              columns (32, 64, 128; the last group of a row may be shorter),
+ *              scale = max(max |y| / top, 2^-126), top = 448 for MQG_Q_E4M3 and 127 for MQG_Q_INT8,
+ *              q = y / scale rounded to nearest, ties to even.  A group that holds a value that is
+ *              not finite has the scale NaN, so that all its values read NaN.
+ *              q: device bytes [cap_rows x q_stride], scale: device float [cap_rows x scale_stride]
+ * A row of zeros gives zeros.  sum, y and q may each be the buffer of x or residual if the strides in bytes are the same.
+ * dim <= MQG_NORM_MAX_DIM.
+ */
+#define MQG_NORM_MAX_DIM 16384
+typedef enum { MQG_Q_E4M3 = 0, MQG_Q_INT8 = 1 } mqg_qtype;
+int mqg_rms_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const float *weight,
+                 float eps, const int64_t *num_rows_dev, int64_t cap_rows, int32_t dim, int32_t dtype, void *sum, int64_t sum_stride,
+                 void *y, int64_t y_stride, void *q, int64_t q_stride, int32_t q_type, int32_t group, float *scale, int64_t scale_stride,
+                 mqg_stream stream);
+
+/*
+ * Its backward.  sum: the forward's s (its x where there was no residual); grad_y: the gradient of y (where y was
+ * read in 8 bits: of the values that these stand for, the rounding is taken as the identity); grad_sum: the gradient that reaches s
+ * by its other uses, NULL if it has none.  With R = 1/sqrt(mean(s^2) + eps):
+ *   grad_x = R (grad_y * weight - s * R^2 mean(grad_y * weight * s)) + grad_sum   (the gradient of x and of residual)
+ *   grad_weight[c] = sum over the rows of grad_y * s * R    (device float [dim], written; NULL if not wanted)
+ * Sums in fp32.  grad_weight is made of one sum per workgroup, added in a fixed order: the same bits in every call of the same
+ * cap_rows, dim, dtype and number of rows.  grad_x may be the buffer of grad_y, grad_sum or sum if its stride is the same.
+ */
+int mqg_rms_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, const void *sum, int64_t sum_stride, const float *weight,
+                          const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows_dev, int64_t cap_rows, int32_t dim,
+                          int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, mqg_stream stream);
+
+/*
+ * mqg_sage_mean_aggregate of source rows in 8 bits with scales, as mqg_rms_norm writes them:
+ *   out[i, c] = (1/n_i) * sum_{e in row i} scale[indices[e], c / group] * q[indices[e], c]
+ *   (group = 0: one scale per row); a destination with no sampled neighbour gets zeros.
+ * q: device bytes [num_src x q_stride]; scale: device float [num_src x scale_stride]; out: device [cap_dst x out_stride] of dtype.
+ * Sums in fp32, in an order that depends on the row's entries, dim and dtype alone; one rounding at the store.  Its backward, for the values that q
+ * stands for, is mqg_sage_mean_aggregate_backward.
+ */
+int mqg_sage_mean_aggregate_q8(mqg_ctx *ctx, const mqg_block *block, const void *q, int64_t q_stride, int32_t q_type, int32_t group,
+                               const float *scale, int64_t scale_stride, void *out, int64_t out_stride, int32_t dim, int32_t dtype,
+                               mqg_stream stream);
+
+/* A stack of num_mats matrices, element (r, c) of matrix i at data + i*mat_stride + r*row_stride + c. */
+typedef struct mqg_matrices {
+    int32_t num_mats, rows, cols;
+    int32_t dtype;                       /* mqg_dtype                                    */
+    void *data;                          /* device                                       */
+    int64_t row_stride, mat_stride;
+} mqg_matrices;
+
+/* How an update is orthogonalised: `steps` steps (1..MQG_ORTH_MAX_STEPS) with coefficients (a, b, c) each (host float [3 * steps],
+ * NULL = 3.4445, -4.7750, 2.0315 in all).  A plan of NULL means 5 such steps and eps = 1e-7. */
+#define MQG_ORTH_MAX_STEPS 32
+#define MQG_ORTH_MAX_SIDE 65536
+#define MQG_ORTH_MAX_MATS 65535
+typedef struct mqg_orth {
+    int32_t steps;
+    float eps;
+    const float *coeffs;
+} mqg_orth;
+
+/*
+ * The orthogonal factor of every matrix of a stack, by Newton-Schulz products: X = U / (|U|_F + eps), then per step
+ *   A = X X^T,  X <- a X + (b A + c A^2) X          (with X^T X where U has more rows than columns)
+ * which takes every singular value x to a x + b x^3 + c x^5 and keeps the singular vectors.  The usual coefficients take singular values
+ * from about 0.001 up to 0.7 .. 1.2 in five steps; smaller ones stay smaller.  Rows and columns of zeros stay zeros; a matrix that holds a value that is not finite
+ * gives one without a finite value.
+ * Products are exact to about 22 bits with sums in fp32, whatever the types.  Coefficients that take singular values of up to
+ * 1 above 256 are refused with MQG_ERR_UNSUPPORTED.
+ *   update   any type;  out  any type, the same sizes; may be the update's buffer if the layout and the type are the same
+ */
+int mqg_orthogonalize(mqg_ctx *ctx, const mqg_matrices *update, const mqg_matrices *out, const mqg_orth *plan, mqg_stream stream);
+
+/*
+ * A step of the weights around it (the momentum's orthogonal factor as the update):
+ *   momentum <- beta * momentum + grad;  U = nesterov ? grad + beta * momentum : momentum
+ *   weight   <- (1 - lr * weight_decay) * weight - lr * scale * orthogonalize(U)
+ * grad: any type; momentum, weight: MQG_F32, read and written in place.  `scale` is the caller's rule for the size of the step
+ * (e.g. sqrt(max(1, rows / cols))).
+ */
+int mqg_muon_step(mqg_ctx *ctx, const mqg_matrices *grad, const mqg_matrices *momentum, const mqg_matrices *weight, float lr, float beta,
+                  int32_t nesterov, float weight_decay, float scale, const mqg_orth *plan, mqg_stream stream);
 
 /*
  * Depth of the mini-batch queue, i.e. how many mini-batches to keep in flight

@@ -3,6 +3,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <new>
 
 #include "common.h"
 
@@ -11,6 +12,17 @@ thread_local std::string g_create_error = "";
 
 bool valid_itype(int32_t t) { return t == MQG_I32 || t == MQG_I64; }
 bool valid_dtype(int32_t t) { return t == MQG_F32 || t == MQG_F16; }
+bool valid_layer_dtype(int32_t t) { return valid_dtype(t) || t == MQG_BF16; }
+
+// No exception leaves the library: a message or a record that finds no memory is an error of the call.
+template <typename F>
+int guarded(F call) {
+    try {
+        return call();
+    } catch (...) {
+        return MQG_ERR_HIP;
+    }
+}
 
 template <typename T>
 hipError_t dev_alloc(T **p, int64_t n) {
@@ -101,6 +113,29 @@ void free_backward_scratch(mqg_ctx *ctx) {
     ctx->bwd = RadixBufs{};
     ctx->bwd_dst_row = ctx->bwd_col_ptr = nullptr;
     ctx->bwd_nnz_cap = ctx->bwd_src_cap = 0;
+}
+
+// Room for what a layer's calls leave between their launches.  Growing it waits for the stream first: earlier work may still use the old one.
+int ensure_layer_scratch(mqg_ctx *ctx, int64_t bytes, hipStream_t s, const char *who) {
+    if (bytes <= ctx->layer_scratch_bytes) return MQG_OK;
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    hipError_t e = hipStreamIsCapturing(s, &capture);
+    if (e != hipSuccess) return fail(ctx, MQG_ERR_HIP, std::string(who) + ": " + hipGetErrorString(e));
+    if (capture != hipStreamCaptureStatusNone)
+        return fail(ctx, MQG_ERR_UNSUPPORTED, std::string(who) + ": needs more scratch than the context has while the stream is recorded (mqg_ctx_reserve_layer)");
+    e = hipStreamSynchronize(s);
+    if (e != hipSuccess) return fail(ctx, MQG_ERR_HIP, std::string(who) + ": " + hipGetErrorString(e));
+    (void)hipFree(ctx->layer_scratch);
+    ctx->layer_scratch = nullptr;
+    ctx->layer_scratch_bytes = 0;
+    e = hipMalloc(reinterpret_cast<void **>(&ctx->layer_scratch), static_cast<size_t>(bytes));
+    if (e != hipSuccess) {
+        ctx->layer_scratch = nullptr;
+        (void)hipGetLastError();
+        return fail(ctx, MQG_ERR_HIP, std::string(who) + ": scratch allocation failed: " + hipGetErrorString(e));
+    }
+    ctx->layer_scratch_bytes = bytes;
+    return MQG_OK;
 }
 
 }  // namespace mqg
@@ -212,6 +247,7 @@ int mqg_ctx_destroy(mqg_ctx *c) {
     (void)hipFree(c->prio_bitmap);
     (void)hipFree(c->prio_count);
     (void)hipFree(c->cache_arena);
+    (void)hipFree(c->layer_scratch);
     for (auto &r : c->prof_recs) {
         (void)hipEventDestroy(r.start);
         (void)hipEventDestroy(r.stop);
@@ -569,6 +605,175 @@ int mqg_weighted_aggregate_backward(mqg_ctx *ctx, const mqg_block *block, const 
     if (go_stride < dim || gx_stride < dim) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_weighted_aggregate_backward: stride below dim");
     return mqg::run_aggregate_backward(ctx, block, edge_w, self_w, grad_out, go_stride, grad_x, gx_stride, dim, dtype,
                                        static_cast<hipStream_t>(stream));
+}
+
+static int check_norm_rows(mqg_ctx *ctx, const char *who, int64_t cap_rows, int32_t dim, int32_t dtype, float eps) {
+    if (!valid_layer_dtype(dtype) || dim < 1) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": bad dtype or dim");
+    if (dim > MQG_NORM_MAX_DIM) return fail(ctx, MQG_ERR_UNSUPPORTED, std::string(who) + ": dim above MQG_NORM_MAX_DIM");
+    if (cap_rows < 0) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": negative cap_rows");
+    if (!(eps >= 0.f) || std::isinf(eps)) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": eps is negative or not a number");
+    return MQG_OK;
+}
+
+static int check_q8(mqg_ctx *ctx, const char *who, int64_t q_stride, int32_t q_type, int32_t group, const float *scale, int64_t scale_stride, int32_t dim) {
+    if (q_type != MQG_Q_E4M3 && q_type != MQG_Q_INT8) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": bad q_type");
+    if (group != 0 && group != 32 && group != 64 && group != 128)
+        return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": group is not 0, 32, 64 or 128");
+    if (!scale) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": scale is NULL");
+    if (q_stride < dim || scale_stride < (group ? mqg::ceil_div(dim, group) : 1))
+        return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": stride below the columns or scales of a row");
+    return MQG_OK;
+}
+
+int mqg_rms_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const float *weight,
+                 float eps, const int64_t *num_rows_dev, int64_t cap_rows, int32_t dim, int32_t dtype, void *sum, int64_t sum_stride,
+                 void *y, int64_t y_stride, void *q, int64_t q_stride, int32_t q_type, int32_t group, float *scale, int64_t scale_stride,
+                 mqg_stream stream) {
+    if (!ctx) return MQG_ERR_INVALID_ARG;
+    return guarded([&]() -> int {
+        int rc = check_norm_rows(ctx, "mqg_rms_norm", cap_rows, dim, dtype, eps);
+        if (rc != MQG_OK) return rc;
+        if (cap_rows > 0 && !y && !q) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_rms_norm: neither y nor q is given");
+        if (cap_rows > 0 && !x) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_rms_norm: x is NULL");
+        if (x_stride < dim || (residual && residual_stride < dim) || (sum && sum_stride < dim) || (y && y_stride < dim))
+            return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_rms_norm: stride below dim");
+        if (q) {
+            rc = check_q8(ctx, "mqg_rms_norm", q_stride, q_type, group, scale, scale_stride, dim);
+            if (rc != MQG_OK) return rc;
+        }
+        return mqg::run_rms_norm(ctx, x, x_stride, residual, residual_stride, weight, eps, num_rows_dev, cap_rows, dim, dtype, sum, sum_stride, y,
+                                 y_stride, q, q_stride, q_type, group, scale, scale_stride, static_cast<hipStream_t>(stream));
+    });
+}
+
+int mqg_rms_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, const void *sum, int64_t sum_stride, const float *weight,
+                          const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows_dev, int64_t cap_rows, int32_t dim,
+                          int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, mqg_stream stream) {
+    if (!ctx) return MQG_ERR_INVALID_ARG;
+    return guarded([&]() -> int {
+        int rc = check_norm_rows(ctx, "mqg_rms_norm_backward", cap_rows, dim, dtype, eps);
+        if (rc != MQG_OK) return rc;
+        if (cap_rows > 0 && (!grad_y || !sum || !grad_x)) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_rms_norm_backward: NULL grad_y, sum or grad_x");
+        if (gy_stride < dim || sum_stride < dim || gx_stride < dim || (grad_sum && gs_stride < dim))
+            return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_rms_norm_backward: stride below dim");
+        return mqg::run_rms_norm_backward(ctx, grad_y, gy_stride, sum, sum_stride, weight, grad_sum, gs_stride, eps, num_rows_dev, cap_rows, dim,
+                                          dtype, grad_x, gx_stride, grad_weight, static_cast<hipStream_t>(stream));
+    });
+}
+
+int mqg_sage_mean_aggregate_q8(mqg_ctx *ctx, const mqg_block *block, const void *q, int64_t q_stride, int32_t q_type, int32_t group,
+                               const float *scale, int64_t scale_stride, void *out, int64_t out_stride, int32_t dim, int32_t dtype,
+                               mqg_stream stream) {
+    if (!ctx) return MQG_ERR_INVALID_ARG;
+    return guarded([&]() -> int {
+        if (!block || !block->indptr || !block->indices || !block->sizes)
+            return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_sage_mean_aggregate_q8: NULL block buffers");
+        if (!valid_layer_dtype(dtype) || dim < 1) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_sage_mean_aggregate_q8: bad dtype or dim");
+        if (dim > (1 << 24)) return fail(ctx, MQG_ERR_UNSUPPORTED, "mqg_sage_mean_aggregate_q8: dim above 2^24");
+        if (block->cap_dst < 0) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_sage_mean_aggregate_q8: negative cap_dst");
+        if (block->cap_dst > 0 && (!q || !out)) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_sage_mean_aggregate_q8: NULL q or out");
+        if (out_stride < dim) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_sage_mean_aggregate_q8: stride below dim");
+        int rc = check_q8(ctx, "mqg_sage_mean_aggregate_q8", q_stride, q_type, group, scale, scale_stride, dim);
+        if (rc != MQG_OK) return rc;
+        return mqg::run_mean_aggregate_q8(ctx, block, q, q_stride, q_type, group, scale, scale_stride, out, out_stride, dim, dtype,
+                                          static_cast<hipStream_t>(stream));
+    });
+}
+
+static int check_matrices(mqg_ctx *ctx, const char *who, const mqg_matrices *m, bool needed_type_only_f32) {
+    if (!m) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": NULL matrices");
+    if (m->num_mats < 0 || m->rows < 0 || m->cols < 0) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": negative size");
+    if (!valid_layer_dtype(m->dtype) || (needed_type_only_f32 && m->dtype != MQG_F32))
+        return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + (needed_type_only_f32 ? ": momentum and weights are MQG_F32" : ": bad dtype"));
+    if (m->num_mats == 0 || m->rows == 0 || m->cols == 0) return MQG_OK;
+    if (!m->data) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": NULL data");
+    if (m->row_stride < m->cols || (m->num_mats > 1 && m->mat_stride < (int64_t(m->rows) - 1) * m->row_stride + m->cols))
+        return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": stride below the columns of a row or the rows of a matrix");
+    return MQG_OK;
+}
+
+static int orth_checked(mqg_ctx *ctx, const char *who, const mqg_matrices *in, const mqg_matrices *momentum, const mqg_matrices *out,
+                        const mqg_orth *plan, mqg::OrthCall *call) {
+    int rc = check_matrices(ctx, who, in, false);
+    if (rc == MQG_OK && momentum) rc = check_matrices(ctx, who, momentum, true);
+    if (rc == MQG_OK) rc = check_matrices(ctx, who, out, momentum != nullptr);
+    if (rc != MQG_OK) return rc;
+    for (const mqg_matrices *m : {momentum, out})
+        if (m && (m->num_mats != in->num_mats || m->rows != in->rows || m->cols != in->cols))
+            return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": matrices of different sizes");
+    if (in->rows > MQG_ORTH_MAX_SIDE || in->cols > MQG_ORTH_MAX_SIDE || in->num_mats > MQG_ORTH_MAX_MATS)
+        return fail(ctx, MQG_ERR_UNSUPPORTED, std::string(who) + ": more than MQG_ORTH_MAX_SIDE rows or columns, or MQG_ORTH_MAX_MATS matrices");
+    static const float usual[3] = {3.4445f, -4.775f, 2.0315f};
+    const int32_t steps = plan ? plan->steps : 5;
+    if (steps < 1 || steps > MQG_ORTH_MAX_STEPS) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": steps outside 1..MQG_ORTH_MAX_STEPS");
+    for (int i = 0; i < steps; ++i)
+        for (int j = 0; j < 3; ++j) call->coeffs[3 * i + j] = plan && plan->coeffs ? plan->coeffs[3 * i + j] : usual[j];
+    if (!mqg::orth_coeffs_fit(call->coeffs, steps))
+        return fail(ctx, MQG_ERR_UNSUPPORTED, std::string(who) + ": the coefficients take singular values of at most 1 above 256");
+    call->eps = plan ? plan->eps : 1e-7f;
+    if (!(call->eps >= 0.f) || std::isinf(call->eps)) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": eps is negative or not a number");
+    call->who = who;
+    call->steps = steps;
+    call->mats = in->num_mats;
+    call->rows = in->rows;
+    call->cols = in->cols;
+    call->grad = in->data;
+    call->grad_row = in->row_stride;
+    call->grad_mat = in->mat_stride;
+    call->dtype = in->dtype;
+    if (momentum) {
+        call->momentum = static_cast<float *>(momentum->data);
+        call->mom_row = momentum->row_stride;
+        call->mom_mat = momentum->mat_stride;
+    }
+    call->out = out->data;
+    call->out_row = out->row_stride;
+    call->out_mat = out->mat_stride;
+    call->out_type = out->dtype;
+    return MQG_OK;
+}
+
+int mqg_orthogonalize(mqg_ctx *ctx, const mqg_matrices *update, const mqg_matrices *out, const mqg_orth *plan, mqg_stream stream) {
+    if (!ctx) return MQG_ERR_INVALID_ARG;
+    return guarded([&]() -> int {
+        mqg::OrthCall call;
+        int rc = orth_checked(ctx, "mqg_orthogonalize", update, nullptr, out, plan, &call);
+        if (rc != MQG_OK) return rc;
+        if (call.mats == 0 || call.rows == 0 || call.cols == 0) return MQG_OK;
+        call.out_by = 1.f;
+        return mqg::run_orthogonalize(ctx, call, static_cast<hipStream_t>(stream));
+    });
+}
+
+int mqg_muon_step(mqg_ctx *ctx, const mqg_matrices *grad, const mqg_matrices *momentum, const mqg_matrices *weight, float lr, float beta,
+                  int32_t nesterov, float weight_decay, float scale, const mqg_orth *plan, mqg_stream stream) {
+    if (!ctx) return MQG_ERR_INVALID_ARG;
+    return guarded([&]() -> int {
+        if (!momentum) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_muon_step: NULL matrices");
+        if (!std::isfinite(lr) || !std::isfinite(beta) || !std::isfinite(weight_decay) || !std::isfinite(scale))
+            return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_muon_step: lr, beta, weight_decay or scale is not finite");
+        mqg::OrthCall call;
+        int rc = orth_checked(ctx, "mqg_muon_step", grad, momentum, weight, plan, &call);
+        if (rc != MQG_OK) return rc;
+        if (call.mats == 0 || call.rows == 0 || call.cols == 0) return MQG_OK;
+        call.beta = beta;
+        call.nesterov = nesterov ? 1 : 0;
+        call.step = 1;
+        call.keep = static_cast<float>(1.0 - static_cast<double>(lr) * weight_decay);
+        call.out_by = static_cast<float>(-static_cast<double>(lr) * scale);
+        return mqg::run_orthogonalize(ctx, call, static_cast<hipStream_t>(stream));
+    });
+}
+
+int mqg_ctx_reserve_layer(mqg_ctx *ctx, int32_t norm_dim, int32_t num_mats, int32_t rows, int32_t cols) {
+    if (!ctx) return MQG_ERR_INVALID_ARG;
+    return guarded([&]() -> int {
+        if (norm_dim < 0 || num_mats < 0 || rows < 0 || cols < 0) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_ctx_reserve_layer: negative size");
+        if (norm_dim > MQG_NORM_MAX_DIM || num_mats > MQG_ORTH_MAX_MATS || rows > MQG_ORTH_MAX_SIDE || cols > MQG_ORTH_MAX_SIDE)
+            return fail(ctx, MQG_ERR_UNSUPPORTED, "mqg_ctx_reserve_layer: above the calls' limits");
+        return mqg::ensure_layer_scratch(ctx, std::max(mqg::norm_scratch_bytes(norm_dim), mqg::orth_scratch_bytes(num_mats, rows, cols)), nullptr,
+                                         "mqg_ctx_reserve_layer");
+    });
 }
 
 int mqg_queue_size(double max_prepare_ms, double mean_compute_ms, int64_t total_mem_bytes, int64_t peak_mem_bytes,

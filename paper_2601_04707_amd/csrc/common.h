@@ -114,6 +114,9 @@ struct mqg_ctx {
     // temporaries of the cache build, reserved by mqg_ctx_reserve (otherwise allocated and freed per call)
     char *cache_arena = nullptr;
     int64_t cache_arena_bytes = 0;
+    // what the calls of a layer leave between their launches (norm.hip, orthogonal.hip); grows with the calls, or by mqg_ctx_reserve_layer
+    char *layer_scratch = nullptr;
+    int64_t layer_scratch_bytes = 0;
     // hash-table dedup (MQG_OPT_DEDUP_HASH); allocated when the option is first used
     bool dedup_hash = false;
     unsigned long long *hash_table = nullptr;      // [hash_capacity] (id << 32 | position), all ones = empty
@@ -198,6 +201,36 @@ int run_select_row_candidates(mqg_ctx *ctx, const uint64_t *keys, const uint32_t
                               int32_t prioritised, int32_t ordered, uint32_t *out_mask, hipStream_t s);
 int run_exp_tickets(mqg_ctx *ctx, uint64_t seed, int64_t tag, int64_t first, int64_t n, uint64_t *tickets, hipStream_t s);
 int run_set_sampling_priority(mqg_ctx *ctx, const mqg_graph *g, const mqg_cache *cache, hipStream_t s);
+// the calls of a layer (norm.hip, aggregate_q8.hip, orthogonal.hip)
+int ensure_layer_scratch(mqg_ctx *ctx, int64_t bytes, hipStream_t s, const char *who);
+int64_t norm_scratch_bytes(int32_t dim);
+int64_t orth_scratch_bytes(int64_t mats, int64_t rows, int64_t cols);
+int run_rms_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const float *weight,
+                 float eps, const int64_t *num_rows, int64_t cap_rows, int32_t dim, int32_t dtype, void *sum, int64_t sum_stride, void *y,
+                 int64_t y_stride, void *q, int64_t q_stride, int32_t q_type, int32_t group, float *scale, int64_t scale_stride, hipStream_t s);
+int run_rms_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, const void *sum, int64_t sum_stride, const float *weight,
+                          const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows, int64_t cap_rows, int32_t dim,
+                          int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, hipStream_t s);
+int run_mean_aggregate_q8(mqg_ctx *ctx, const mqg_block *b, const void *q, int64_t q_stride, int32_t q_type, int32_t group, const float *scale,
+                          int64_t scale_stride, void *out, int64_t out_stride, int32_t dim, int32_t dtype, hipStream_t s);
+struct OrthCall {
+    const char *who = "";
+    int64_t mats = 0, rows = 0, cols = 0;
+    const void *grad = nullptr;
+    int64_t grad_row = 0, grad_mat = 0;      // strides in elements: of a row, of a matrix
+    float *momentum = nullptr;               // null: the gradient itself is orthogonalised
+    int64_t mom_row = 0, mom_mat = 0;
+    int32_t dtype = 0, nesterov = 0;
+    float beta = 0.f, eps = 0.f;
+    int32_t steps = 0;
+    float coeffs[3 * MQG_ORTH_MAX_STEPS] = {0.f};
+    void *out = nullptr;                     // out = out_by * X, or, with step, out = keep * out + out_by * X in float
+    int64_t out_row = 0, out_mat = 0;
+    int32_t out_type = 0, step = 0;
+    float keep = 0.f, out_by = 0.f;
+};
+bool orth_coeffs_fit(const float *coeffs, int32_t steps);
+int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s);
 // hash-table dedup (dedup_hash.hip)
 int ensure_hash_scratch(mqg_ctx *ctx);
 void free_hash_scratch(mqg_ctx *ctx);

@@ -1,0 +1,437 @@
+// Root-mean-square norm of the rows between two layers, with the residual's addition and an output in 8 bits, and its backward.
+//
+//   forward    s = x + r,  y = s rsqrt(mean(s^2) + eps) w,  8 bits: scale = max(max|y| / top, 2^-126) per row or group of columns,
+//              q = y / scale rounded to nearest even (top = 448: e4m3, 127: int8)
+//   backward   with R = rsqrt(mean(s^2) + eps) and c = R^2 mean(gy w s):  gx = R (gy w - c s) + gs,  gw = sum over rows of gy s R
+//
+// Both are bound by memory: every input is read once and every output written once, a row stays in registers in between.  A row
+// is the work of 4 to 64 lanes of a wavefront, of four wavefronts or of sixteen, by its length: as few as hold it with up to
+// four vectors of 16 bytes each, so that a reduction over the row is a few exchanges between lanes and rows that are
+// short fill the wavefront.
+#include <algorithm>
+
+#include "common.h"
+#include "layer_types.h"
+
+namespace mqg {
+
+constexpr int kNormParts = 1024;      // workgroups of a backward at most
+
+int64_t norm_scratch_bytes(int32_t dim) { return int64_t(kNormParts) * dim * int64_t(sizeof(float)); }
+
+namespace {
+
+struct NormArgs {
+    const void *x, *residual;
+    const float *weight;
+    const int64_t *num_rows;
+    void *sum, *y;
+    uint8_t *q;
+    float *scale;
+    int64_t x_stride, residual_stride, sum_stride, y_stride, q_stride, scale_stride;
+    int64_t cap_rows;
+    float eps;
+    int32_t dim, q_type, group;       // group: columns per scale, 0 = the row
+};
+
+__device__ __forceinline__ int64_t rows_of(const int64_t *num_rows, int64_t cap) {
+    if (!num_rows) return cap;
+    const int64_t n = *num_rows;
+    return n < cap ? (n > 0 ? n : 0) : cap;
+}
+
+// What the lanes of a row find together.  Rows of several wavefronts exchange through LDS: two buffers in turn, so that one barrier
+// per exchange is enough (who writes a buffer again has passed the barrier behind which all have read it).
+template <int LANES>
+struct RowLanes {
+    static constexpr int kWaves = LANES / kWave;
+    float *lds;
+    int turn = 0;
+    __device__ __forceinline__ explicit RowLanes(float *l) : lds(l) {}
+    template <typename F>
+    __device__ __forceinline__ float join(float v, F f) {
+        float *buf = lds + turn * kWaves;
+        turn ^= 1;
+        if (lane_id() == 0) buf[threadIdx.x >> 6] = v;
+        __syncthreads();
+        float all = buf[0];
+#pragma unroll
+        for (int k = 1; k < kWaves; ++k) all = f(all, buf[k]);
+        return all;
+    }
+    __device__ __forceinline__ float sum(float v) {
+        v = lanes_sum(v, LANES < kWave ? LANES : kWave);
+        if constexpr (LANES > kWave) v = join(v, [](float a, float b) { return a + b; });
+        return v;
+    }
+    __device__ __forceinline__ uint32_t max(uint32_t v) {
+        v = lanes_max(v, LANES < kWave ? LANES : kWave);
+        if constexpr (LANES > kWave)
+            v = __float_as_uint(join(__uint_as_float(v), [](float a, float b) { return __uint_as_float(max_u32(__float_as_uint(a), __float_as_uint(b))); }));
+        return v;
+    }
+};
+
+// The scale of a group whose largest |y| has the bit pattern `most` (patterns of absolute values order as the values do, with infinity and NaN
+// above all others: a group that holds one has the scale NaN, so that all its values read NaN).
+__device__ __forceinline__ float scale_of(uint32_t most, float top) {
+    if (most >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
+    const float s = __uint_as_float(most) / top;
+    return s > 0x1p-126f ? s : 0x1p-126f;
+}
+
+// V values of a row divided by their scale, in 8 bits
+template <int V>
+__device__ __forceinline__ void store_q(uint8_t *row, int i, int dim, const float (&y)[V], float scale, int q_type) {
+    const float inv = 1.0f / scale;
+    uint32_t w[V / 4];
+    if (q_type == MQG_Q_E4M3) {
+#pragma unroll
+        for (int k = 0; k < V / 4; ++k) {
+            int p = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k] * inv, y[4 * k + 1] * inv, 0, false);
+            w[k] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2] * inv, y[4 * k + 3] * inv, p, true));
+        }
+    } else {
+        const bool number = scale == scale;
+#pragma unroll
+        for (int k = 0; k < V / 4; ++k) {
+            w[k] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int v = number ? static_cast<int>(rintf(y[4 * k + j] * inv)) : 0;
+                w[k] |= (static_cast<uint32_t>(v) & 0xFFu) << (8 * j);
+            }
+        }
+    }
+    if ((i + 1) * V <= dim) {
+        typedef uint32_t Words __attribute__((ext_vector_type(V / 4)));
+        typedef Words AnyWords __attribute__((aligned(1)));
+        Words v;
+#pragma unroll
+        for (int k = 0; k < V / 4; ++k) {
+            if constexpr (V == 4) v = w[k];
+            else v[k] = w[k];
+        }
+        *reinterpret_cast<AnyWords *>(row + i * V) = v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (i * V + j < dim) row[i * V + j] = static_cast<uint8_t>(w[j / 4] >> (8 * (j % 4)));
+    }
+}
+
+template <typename T, int LANES, int NV>
+__global__ void __launch_bounds__(LANES > kBlock ? LANES : kBlock)
+k_rms_norm(NormArgs a) {
+    constexpr int V = Vec<T>::kLen;
+    constexpr int kThreads = LANES > kBlock ? LANES : kBlock;
+    constexpr int kRows = kThreads / LANES;                // rows of a workgroup
+    __shared__ float lds[LANES > kWave ? 2 * (LANES / kWave) : 1];
+    RowLanes<LANES> lanes(lds);
+    const int lane = static_cast<int>(threadIdx.x) % LANES;
+    const int64_t n = rows_of(a.num_rows, a.cap_rows);
+    const int dim = a.dim;
+    const float top = a.q_type == MQG_Q_E4M3 ? 448.f : 127.f;
+    const int group_lanes = a.group / V;                   // lanes that share a scale, 0 = the row's
+    float w[NV][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c = (k * LANES + lane) * V + j;
+            w[k][j] = !a.weight ? 1.f : c < dim ? a.weight[c] : 0.f;
+        }
+    for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; row < n; row += int64_t(gridDim.x) * kRows) {
+        float s[NV][V];
+        const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) load_vec(x, k * LANES + lane, dim, s[k]);
+        if (a.residual) {
+            const T *r = static_cast<const T *>(a.residual) + row * a.residual_stride;
+            float t[NV][V];
+#pragma unroll
+            for (int k = 0; k < NV; ++k) load_vec(r, k * LANES + lane, dim, t[k]);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) s[k][j] += t[k][j];
+        }
+        if (a.sum) {
+            T *sum = static_cast<T *>(a.sum) + row * a.sum_stride;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) store_vec(sum, k * LANES + lane, dim, s[k]);
+        }
+        float squares = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float part = 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) part += s[k][j] * s[k][j];
+            squares += part;
+        }
+        squares = lanes.sum(squares);
+        const float r = 1.0f / sqrtf(squares / static_cast<float>(dim) + a.eps);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[k][j] = s[k][j] * r * w[k][j];
+        if (a.y) {
+            T *y = static_cast<T *>(a.y) + row * a.y_stride;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) store_vec(y, k * LANES + lane, dim, s[k]);
+        }
+        if (!a.q) continue;
+        uint8_t *q = a.q + row * a.q_stride;
+        float *scale = a.scale + row * a.scale_stride;
+        uint32_t most[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            most[k] = 0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) most[k] = max_u32(most[k], __float_as_uint(s[k][j]) & 0x7FFFFFFFu);
+        }
+        if (group_lanes == 0) {
+            uint32_t m = most[0];
+#pragma unroll
+            for (int k = 1; k < NV; ++k) m = max_u32(m, most[k]);
+            const float sc = scale_of(lanes.max(m), top);
+            if (lane == 0) scale[0] = sc;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) store_q(q, k * LANES + lane, dim, s[k], sc, a.q_type);
+        } else {
+            const int width = group_lanes < LANES ? group_lanes : LANES;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const float sc = scale_of(lanes_max(most[k], width), top);
+                const int i = k * LANES + lane;
+                if (lane % width == 0 && i * V < dim) scale[i / group_lanes] = sc;
+                store_q(q, i, dim, s[k], sc, a.q_type);
+            }
+        }
+    }
+}
+
+struct NormGradArgs {
+    const void *grad_y, *s, *grad_sum;
+    const float *weight;
+    const int64_t *num_rows;
+    void *grad_x;
+    float *parts;                     // [grid x dim] every workgroup's share of the weight's gradient; null if that is not wanted
+    int64_t gy_stride, s_stride, gs_stride, gx_stride;
+    int64_t cap_rows;
+    float eps;
+    int32_t dim;
+};
+
+template <typename T, int LANES, int NV>
+__global__ void __launch_bounds__(LANES > kBlock ? LANES : kBlock)
+k_rms_norm_backward(NormGradArgs a) {
+    constexpr int V = Vec<T>::kLen;
+    constexpr int kThreads = LANES > kBlock ? LANES : kBlock;
+    constexpr int kRows = kThreads / LANES;
+    constexpr int kCols = LANES * NV * V;
+    // rows of several wavefronts: their exchange; others: the wavefronts' sums of the weight's gradient
+    __shared__ float lds[LANES > kWave ? 2 * (LANES / kWave) : kWavesPerBlock * kCols];
+    RowLanes<LANES> lanes(lds);
+    const int lane = static_cast<int>(threadIdx.x) % LANES;
+    const int64_t n = rows_of(a.num_rows, a.cap_rows);
+    const int dim = a.dim;
+    float w[NV][V], gw[NV][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c = (k * LANES + lane) * V + j;
+            w[k][j] = !a.weight ? 1.f : c < dim ? a.weight[c] : 0.f;
+            gw[k][j] = 0.f;
+        }
+    for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; row < n; row += int64_t(gridDim.x) * kRows) {
+        float s[NV][V], g[NV][V];
+        const T *sr = static_cast<const T *>(a.s) + row * a.s_stride;
+        const T *gr = static_cast<const T *>(a.grad_y) + row * a.gy_stride;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            load_vec(sr, k * LANES + lane, dim, s[k]);
+            load_vec(gr, k * LANES + lane, dim, g[k]);
+        }
+        float squares = 0.f, dot = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float p = 0.f, d = 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                p += s[k][j] * s[k][j];
+                d += g[k][j] * w[k][j] * s[k][j];
+            }
+            squares += p;
+            dot += d;
+        }
+        squares = lanes.sum(squares);
+        dot = lanes.sum(dot);
+        const float r = 1.0f / sqrtf(squares / static_cast<float>(dim) + a.eps);
+        const float c = r * r * (dot / static_cast<float>(dim));
+        if (a.parts) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) gw[k][j] += g[k][j] * (s[k][j] * r);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) g[k][j] = r * (g[k][j] * w[k][j] - c * s[k][j]);
+        if (a.grad_sum) {
+            const T *gs = static_cast<const T *>(a.grad_sum) + row * a.gs_stride;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                load_vec(gs, k * LANES + lane, dim, s[k]);
+#pragma unroll
+                for (int j = 0; j < V; ++j) g[k][j] += s[k][j];
+            }
+        }
+        T *gx = static_cast<T *>(a.grad_x) + row * a.gx_stride;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) store_vec(gx, k * LANES + lane, dim, g[k]);
+    }
+    if (!a.parts) return;
+    float *part = a.parts + int64_t(blockIdx.x) * dim;
+    if constexpr (LANES > kWave) {                         // the workgroup is one row's: nothing to join
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int col = (k * LANES + lane) * V + j;
+                if (col < dim) part[col] = gw[k][j];
+            }
+    } else {
+        const int wave = static_cast<int>(threadIdx.x) >> 6;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float v = gw[k][j];
+#pragma unroll
+                for (int off = LANES; off < kWave; off <<= 1) v += __shfl_xor(v, off, kWave);
+                if (lane_id() < LANES) lds[wave * kCols + (k * LANES + lane) * V + j] = v;
+            }
+        __syncthreads();
+        for (int col = static_cast<int>(threadIdx.x); col < dim; col += kThreads) {
+            float v = lds[col];
+#pragma unroll
+            for (int k = 1; k < kWavesPerBlock; ++k) v += lds[k * kCols + col];
+            part[col] = v;
+        }
+    }
+}
+
+// out[c] = sum over the parts, 16 columns a workgroup: 16 threads take a column's parts in turn and their sums are added in order.
+constexpr int kSumCols = 16;
+__global__ void __launch_bounds__(kBlock)
+k_sum_parts(const float *__restrict__ parts, int num_parts, int dim, float *__restrict__ out) {
+    constexpr int kTurns = kBlock / kSumCols;
+    __shared__ float lds[kTurns][kSumCols];
+    const int c = static_cast<int>(blockIdx.x) * kSumCols + static_cast<int>(threadIdx.x) % kSumCols;
+    const int turn = static_cast<int>(threadIdx.x) / kSumCols;
+    float v = 0.f;
+    if (c < dim)
+        for (int p = turn; p < num_parts; p += kTurns) v += parts[int64_t(p) * dim + c];
+    lds[turn][threadIdx.x % kSumCols] = v;
+    __syncthreads();
+    if (turn == 0 && c < dim) {
+        v = lds[0][threadIdx.x];
+#pragma unroll
+        for (int k = 1; k < kTurns; ++k) v += lds[k][threadIdx.x];
+        out[c] = v;
+    }
+}
+
+// How a row is laid out: lanes, and vectors per lane
+struct RowShape {
+    int lanes, nv;
+};
+RowShape row_shape(int dim, int vec) {
+    const int vecs = static_cast<int>(ceil_div(dim, vec));
+    for (int lanes = 4; lanes <= kWave; lanes <<= 1)
+        if (vecs <= lanes) return {lanes, 1};
+    if (vecs <= 4 * kWave) return {kWave, static_cast<int>(ceil_div(vecs, kWave))};
+    if (vecs <= 4 * 256) return {256, vecs <= 2 * 256 ? 2 : 4};
+    return {1024, vecs <= 2 * 1024 ? 2 : 4};
+}
+
+#define MQG_NORM_SHAPES(T, GO)                                     \
+    switch (sh.lanes) {                                            \
+        case 4: GO(T, 4, 1); break;                                \
+        case 8: GO(T, 8, 1); break;                                \
+        case 16: GO(T, 16, 1); break;                              \
+        case 32: GO(T, 32, 1); break;                              \
+        case 64:                                                   \
+            if (sh.nv == 1) GO(T, 64, 1);                          \
+            else if (sh.nv == 2) GO(T, 64, 2);                     \
+            else if (sh.nv == 3) GO(T, 64, 3);                     \
+            else GO(T, 64, 4);                                     \
+            break;                                                 \
+        case 256:                                                  \
+            if (sh.nv == 2) GO(T, 256, 2);                         \
+            else GO(T, 256, 4);                                    \
+            break;                                                 \
+        default:                                                   \
+            if (sh.nv == 2) GO(T, 1024, 2);                        \
+            else if constexpr (sizeof(T) == 4) GO(T, 1024, 4);     \
+    }
+
+template <typename T>
+int launch_norm(mqg_ctx *ctx, const NormArgs &a, hipStream_t s) {
+    const RowShape sh = row_shape(a.dim, Vec<T>::kLen);
+    const int threads = std::max(sh.lanes, kBlock);
+    const int grid = static_cast<int>(std::min<int64_t>(ceil_div(a.cap_rows, threads / sh.lanes), int64_t(256) * 8 * kBlock / threads));
+#define MQG_GO(T, L, N) MQG_LAUNCH(ctx, "k_rms_norm", s, (k_rms_norm<T, L, N><<<grid, threads, 0, s>>>(a)))
+    MQG_NORM_SHAPES(T, MQG_GO)
+#undef MQG_GO
+    return MQG_OK;
+}
+
+template <typename T>
+int launch_norm_backward(mqg_ctx *ctx, NormGradArgs a, float *grad_weight, hipStream_t s) {
+    const RowShape sh = row_shape(a.dim, Vec<T>::kLen);
+    const int threads = std::max(sh.lanes, kBlock);
+    const int grid = static_cast<int>(std::min<int64_t>(ceil_div(a.cap_rows, threads / sh.lanes), sh.lanes > kBlock ? kNormParts / 2 : kNormParts));
+    if (grad_weight) {
+        int rc = ensure_layer_scratch(ctx, norm_scratch_bytes(a.dim), s, "mqg_rms_norm_backward");
+        if (rc != MQG_OK) return rc;
+        a.parts = reinterpret_cast<float *>(ctx->layer_scratch);
+    }
+#define MQG_GO(T, L, N) MQG_LAUNCH(ctx, "k_rms_norm_backward", s, (k_rms_norm_backward<T, L, N><<<grid, threads, 0, s>>>(a)))
+    if (grid > 0) {
+        MQG_NORM_SHAPES(T, MQG_GO)
+    }
+#undef MQG_GO
+    if (grad_weight)
+        MQG_LAUNCH(ctx, "k_sum_parts", s,
+                   (k_sum_parts<<<static_cast<int>(ceil_div(a.dim, kSumCols)), kBlock, 0, s>>>(a.parts, grid, a.dim, grad_weight)));
+    return MQG_OK;
+}
+#undef MQG_NORM_SHAPES
+
+}  // namespace
+
+int run_rms_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const float *weight,
+                 float eps, const int64_t *num_rows, int64_t cap_rows, int32_t dim, int32_t dtype, void *sum, int64_t sum_stride, void *y,
+                 int64_t y_stride, void *q, int64_t q_stride, int32_t q_type, int32_t group, float *scale, int64_t scale_stride, hipStream_t s) {
+    if (cap_rows == 0) return MQG_OK;
+    const NormArgs a{x, residual, weight, num_rows, sum, y, static_cast<uint8_t *>(q), scale, x_stride, residual_stride, sum_stride,
+                     y_stride, q_stride, scale_stride, cap_rows, eps, dim, q_type, group};
+    if (dtype == MQG_F16) return launch_norm<F16>(ctx, a, s);
+    if (dtype == MQG_BF16) return launch_norm<BF16>(ctx, a, s);
+    return launch_norm<float>(ctx, a, s);
+}
+
+int run_rms_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, const void *sum, int64_t sum_stride, const float *weight,
+                          const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows, int64_t cap_rows, int32_t dim,
+                          int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, hipStream_t s) {
+    const NormGradArgs a{grad_y, sum, grad_sum, weight, num_rows, grad_x, nullptr, gy_stride, sum_stride, gs_stride, gx_stride, cap_rows, eps, dim};
+    if (dtype == MQG_F16) return launch_norm_backward<F16>(ctx, a, grad_weight, s);
+    if (dtype == MQG_BF16) return launch_norm_backward<BF16>(ctx, a, grad_weight, s);
+    return launch_norm_backward<float>(ctx, a, grad_weight, s);
+}
+
+}  // namespace mqg

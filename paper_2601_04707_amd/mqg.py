@@ -19,7 +19,10 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libmqg.so")
 
 MQG_OK, MQG_ERR_INVALID_ARG, MQG_ERR_CAPACITY, MQG_ERR_HIP, MQG_ERR_UNSUPPORTED = 0, -1, -2, -3, -4
-MQG_F32, MQG_F16 = 0, 1
+MQG_F32, MQG_F16, MQG_BF16 = 0, 1, 2
+MQG_Q_E4M3, MQG_Q_INT8 = 0, 1
+MQG_NORM_MAX_DIM = 16384
+MQG_ORTH_MAX_STEPS, MQG_ORTH_MAX_SIDE, MQG_ORTH_MAX_MATS = 32, 65536, 65535
 MQG_I32, MQG_I64 = 0, 1
 MQG_OPT_FORCE_SLOW_SELECT, MQG_OPT_PROFILE, MQG_OPT_MISS_INFLIGHT_BYTES, MQG_OPT_HEAVY_DEGREE, MQG_OPT_DEDUP_HASH = 1, 2, 3, 4, 5
 MQG_OPT_LAYERWISE_CANDIDATES = 6
@@ -35,7 +38,8 @@ EXPORTS = [
     "mqg_weighted_aggregate_backward", "mqg_ctx_set_sampling_priority", "mqg_sample_layerwise",
     "mqg_select_smallest_keys", "mqg_select_row_candidates", "mqg_sample_blocks_seed_dev",
     "mqg_gather_features_static", "mqg_exp_tickets", "mqg_gather_features_cached", "mqg_gather_features_missed",
-    "mqg_ctx_reserve",
+    "mqg_ctx_reserve", "mqg_ctx_reserve_layer", "mqg_rms_norm", "mqg_rms_norm_backward", "mqg_sage_mean_aggregate_q8",
+    "mqg_orthogonalize", "mqg_muon_step",
 ]
 
 if not os.path.exists(LIB_PATH):
@@ -67,6 +71,15 @@ class CCachePlan(ctypes.Structure):
     _fields_ = [("policy", _i32), ("num_steps", _i32), ("seed", ctypes.c_uint64), ("train_ids", _vp),
                 ("num_train", _i64), ("step_fanouts", ctypes.POINTER(_i32)), ("scores_out", _vp),
                 ("walk_form", _i32), ("graph_symmetric", _i32)]
+
+
+class CMatrices(ctypes.Structure):
+    _fields_ = [("num_mats", _i32), ("rows", _i32), ("cols", _i32), ("dtype", _i32), ("data", _vp),
+                ("row_stride", _i64), ("mat_stride", _i64)]
+
+
+class COrth(ctypes.Structure):
+    _fields_ = [("steps", _i32), ("eps", ctypes.c_float), ("coeffs", ctypes.POINTER(ctypes.c_float))]
 
 
 lib.mqg_version.restype = _i32
@@ -133,6 +146,23 @@ lib.mqg_queue_size.argtypes = [ctypes.c_double, ctypes.c_double, _i64, _i64, _i3
                                ctypes.POINTER(_i64)]
 
 
+_f32 = ctypes.c_float
+lib.mqg_ctx_reserve_layer.restype = ctypes.c_int
+lib.mqg_ctx_reserve_layer.argtypes = [_vp, _i32, _i32, _i32, _i32]
+lib.mqg_rms_norm.restype = ctypes.c_int
+lib.mqg_rms_norm.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _f32, _vp, _i64, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _vp,
+                             _i64, _vp]
+lib.mqg_rms_norm_backward.restype = ctypes.c_int
+lib.mqg_rms_norm_backward.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _f32, _vp, _i64, _i32, _i32, _vp, _i64, _vp, _vp]
+lib.mqg_sage_mean_aggregate_q8.restype = ctypes.c_int
+lib.mqg_sage_mean_aggregate_q8.argtypes = [_vp, ctypes.POINTER(CBlock), _vp, _i64, _i32, _i32, _vp, _i64, _vp, _i64, _i32, _i32, _vp]
+lib.mqg_orthogonalize.restype = ctypes.c_int
+lib.mqg_orthogonalize.argtypes = [_vp, ctypes.POINTER(CMatrices), ctypes.POINTER(CMatrices), ctypes.POINTER(COrth), _vp]
+lib.mqg_muon_step.restype = ctypes.c_int
+lib.mqg_muon_step.argtypes = [_vp, ctypes.POINTER(CMatrices), ctypes.POINTER(CMatrices), ctypes.POINTER(CMatrices), _f32, _f32, _i32, _f32, _f32,
+                              ctypes.POINTER(COrth), _vp]
+
+
 class MqgError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"mqg error {code}: {msg}")
@@ -153,6 +183,24 @@ def _dtype(t: torch.Tensor) -> int:
     if t.dtype == torch.float16:
         return MQG_F16
     raise TypeError(f"features must be float32 or float16, got {t.dtype}")
+
+
+_LAYER_DTYPES = {torch.float32: MQG_F32, torch.float16: MQG_F16, torch.bfloat16: MQG_BF16}
+_Q_TYPES = {torch.float8_e4m3fn: MQG_Q_E4M3, torch.int8: MQG_Q_INT8}
+
+
+def _layer_dtype(t: torch.Tensor) -> int:
+    try:
+        return _LAYER_DTYPES[t.dtype]
+    except KeyError:
+        raise TypeError(f"rows and matrices of a layer must be float32, float16 or bfloat16, got {t.dtype}") from None
+
+
+def _q_type(t: torch.Tensor) -> int:
+    try:
+        return _Q_TYPES[t.dtype]
+    except KeyError:
+        raise TypeError(f"8-bit rows must be float8_e4m3fn or int8, got {t.dtype}") from None
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -209,6 +257,11 @@ class Context:
     def reserve(self, what: int, layerwise_rows: int = 0):
         """Allocate optional-path scratch now (a sum of MQG_RESERVE_*)."""
         self.check(lib.mqg_ctx_reserve(self.h, what, layerwise_rows))
+
+    def reserve_layer(self, norm_dim: int = 0, num_mats: int = 0, rows: int = 0, cols: int = 0):
+        """Allocate now the scratch of a layer's calls: mqg_rms_norm_backward for rows of up to norm_dim columns,
+        mqg_orthogonalize and mqg_muon_step for stacks of num_mats matrices of rows x cols."""
+        self.check(lib.mqg_ctx_reserve_layer(self.h, norm_dim, num_mats, rows, cols))
 
     def set_sampling_priority(self, cache, stream=None):
         """Draw cached neighbours first (cache: a Cache, or None for the uniform draw)."""
@@ -275,6 +328,21 @@ class Blocks:
     def host_sizes(self):
         """[(num_dst, num_src, nnz, flags)] - synchronises."""
         return [tuple(int(x) for x in row) for row in self.sizes.cpu().tolist()]
+
+
+class BlockView:
+    """One block (number 0) over tensors that the caller has: indptr and indices int32, sizes int64 [4] on the device,
+    num_src the number of source rows."""
+
+    def __init__(self, indptr: torch.Tensor, indices: torch.Tensor, sizes: torch.Tensor, num_src: int):
+        assert indptr.is_cuda and indptr.dtype == torch.int32 and indptr.is_contiguous() and indptr.numel() >= 1
+        assert indices.is_cuda and indices.dtype == torch.int32 and indices.is_contiguous()
+        assert sizes.is_cuda and sizes.dtype == torch.int64 and sizes.is_contiguous() and sizes.numel() >= 4
+        self.L = 1
+        self.indptr, self.indices, self.sizes = [indptr], [indices], sizes.view(-1, 4)
+        self.bounds = [(indptr.numel() - 1, int(num_src), indices.numel())]
+        self.c = (CBlock * 1)(CBlock(indptr.numel() - 1, int(num_src), indices.numel(), None, indptr.data_ptr(), indices.data_ptr(),
+                                     sizes.data_ptr()))
 
 
 class LayerwiseBlocks(Blocks):
@@ -519,6 +587,116 @@ def mqg_weighted_aggregate_backward(ctx: Context, blocks: Blocks, l: int, edge_w
     ctx.check(lib.mqg_weighted_aggregate_backward(ctx.h, ctypes.byref(blocks.c[l]), ew, sw, grad_out.data_ptr(),
                                                   grad_out.stride(0), grad_x.data_ptr(), grad_x.stride(0),
                                                   grad_x.shape[1], _dtype(grad_x), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------- the calls of a layer
+
+def _rows(t: torch.Tensor, dtype, shape) -> int:
+    """The row stride of a [rows, dim] tensor, checked."""
+    assert t.is_cuda and t.dtype == dtype and t.shape == shape, f"expected {tuple(shape)} of {dtype} on the GPU, got {tuple(t.shape)} of {t.dtype}"
+    assert t.stride(1) == 1 or shape[1] == 1
+    return t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
+
+
+def _norm_inputs(weight, num_rows, dim):
+    if weight is not None:
+        assert weight.is_cuda and weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == dim
+    if num_rows is not None:
+        assert num_rows.is_cuda and num_rows.dtype == torch.int64 and num_rows.numel() >= 1
+
+
+def _scales(q, q_scale, group, shape):
+    assert q_scale is not None and q_scale.is_cuda and q_scale.dtype == torch.float32 and q_scale.dim() == 2
+    assert q_scale.shape[0] >= shape[0] and (q_scale.shape[1] <= 1 or q_scale.stride(1) == 1)
+    per_row = -(-shape[1] // group) if group else 1
+    assert q_scale.shape[1] >= per_row, f"{per_row} scales per row are wanted, got {q_scale.shape[1]}"
+    return q_scale.stride(0) if q_scale.shape[0] > 1 else max(q_scale.stride(0), per_row)
+
+
+def mqg_rms_norm(ctx: Context, x: torch.Tensor, weight: Optional[torch.Tensor] = None, *, residual: Optional[torch.Tensor] = None,
+                 sum_out: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                 q_scale: Optional[torch.Tensor] = None, group: int = 0, eps: float = 1e-6, num_rows: Optional[torch.Tensor] = None,
+                 stream=None) -> None:
+    """y = (x + residual) / rms * weight, row by row; q and q_scale receive it in 8 bits (float8_e4m3fn or int8), one scale
+    per row or per `group` columns; sum_out receives x + residual.  num_rows: device int64, rows past it are left alone."""
+    shape, dtype = x.shape, x.dtype
+    assert x.dim() == 2
+    xs = _rows(x, dtype, shape)
+    rs = _rows(residual, dtype, shape) if residual is not None else 0
+    ss = _rows(sum_out, dtype, shape) if sum_out is not None else 0
+    ys = _rows(y, dtype, shape) if y is not None else 0
+    _norm_inputs(weight, num_rows, shape[1])
+    qs = qt = cs = 0
+    if q is not None:
+        qt, qs, cs = _q_type(q), _rows(q, q.dtype, shape), _scales(q, q_scale, group, shape)
+    ctx.check(lib.mqg_rms_norm(ctx.h, x.data_ptr(), xs, _ptr(residual), rs, _ptr(weight), eps, _ptr(num_rows), shape[0], shape[1],
+                               _layer_dtype(x), _ptr(sum_out), ss, _ptr(y), ys, _ptr(q), qs, qt, group, _ptr(q_scale) if q is not None else None, cs,
+                               _stream(stream)))
+
+
+def mqg_rms_norm_backward(ctx: Context, grad_y: torch.Tensor, s: torch.Tensor, weight: Optional[torch.Tensor], grad_x: torch.Tensor, *,
+                          grad_weight: Optional[torch.Tensor] = None, grad_sum: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                          num_rows: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradient of mqg_rms_norm at the stored sum s (x where there was no residual): grad_x, the same for x and residual, and
+    grad_weight ([dim] float32, written).  grad_sum: the gradient that reaches s by its other uses."""
+    shape, dtype = s.shape, s.dtype
+    assert s.dim() == 2
+    ss, gys, gxs = _rows(s, dtype, shape), _rows(grad_y, dtype, shape), _rows(grad_x, dtype, shape)
+    gss = _rows(grad_sum, dtype, shape) if grad_sum is not None else 0
+    _norm_inputs(weight, num_rows, shape[1])
+    if grad_weight is not None:
+        assert grad_weight.is_cuda and grad_weight.dtype == torch.float32 and grad_weight.is_contiguous() and grad_weight.numel() == shape[1]
+    ctx.check(lib.mqg_rms_norm_backward(ctx.h, grad_y.data_ptr(), gys, s.data_ptr(), ss, _ptr(weight), _ptr(grad_sum), gss, eps, _ptr(num_rows),
+                                        shape[0], shape[1], _layer_dtype(s), grad_x.data_ptr(), gxs, _ptr(grad_weight), _stream(stream)))
+
+
+def mqg_sage_mean_aggregate_q8(ctx: Context, blocks, l: int, q: torch.Tensor, q_scale: torch.Tensor, out: torch.Tensor, *, group: int = 0,
+                               stream=None) -> None:
+    """mqg_sage_mean_aggregate of source rows in 8 bits with scales, as mqg_rms_norm writes them; out: float32, float16 or bfloat16."""
+    assert q.dim() == 2 and out.dim() == 2 and q.shape[0] >= blocks.bounds[l][1] and out.shape[0] >= blocks.bounds[l][0]
+    assert q.shape[1] == out.shape[1]
+    qs, cs, os_ = _rows(q, q.dtype, q.shape), _scales(q, q_scale, group, q.shape), _rows(out, out.dtype, out.shape)
+    ctx.check(lib.mqg_sage_mean_aggregate_q8(ctx.h, ctypes.byref(blocks.c[l]), q.data_ptr(), qs, _q_type(q), group, q_scale.data_ptr(), cs,
+                                             out.data_ptr(), os_, out.shape[1], _layer_dtype(out), _stream(stream)))
+
+
+def _matrices(t: torch.Tensor) -> CMatrices:
+    """A [rows, cols] matrix or a [mats, rows, cols] stack of them, rows contiguous."""
+    assert t.is_cuda and t.dim() in (2, 3)
+    m, (r, c) = (1, t.shape) if t.dim() == 2 else (t.shape[0], t.shape[1:])
+    assert c <= 1 or t.stride(-1) == 1
+    rs = t.stride(-2) if r > 1 else max(t.stride(-2), c)
+    return CMatrices(m, r, c, _layer_dtype(t), t.data_ptr(), rs, t.stride(0) if t.dim() == 3 and m > 1 else rs * r)
+
+
+def _orth(steps, coeffs, eps) -> COrth:
+    """coeffs: None, one (a, b, c) for all steps, or one for each."""
+    if coeffs is None:
+        return COrth(steps, eps, None)
+    flat = [float(v) for row in coeffs for v in row] if hasattr(coeffs[0], "__len__") else [float(v) for v in coeffs] * steps
+    assert len(flat) == 3 * steps, "coeffs: (a, b, c), or one such triple for each step"
+    return COrth(steps, eps, (_f32 * len(flat))(*flat))
+
+
+def mqg_orthogonalize(ctx: Context, update: torch.Tensor, out: torch.Tensor, *, steps: int = 5, coeffs=None, eps: float = 1e-7,
+                      stream=None) -> None:
+    """out = the orthogonal factor of every matrix of `update` ([rows, cols] or [mats, rows, cols]), by Newton-Schulz steps."""
+    assert update.shape == out.shape
+    u, o, p = _matrices(update), _matrices(out), _orth(steps, coeffs, eps)
+    ctx.check(lib.mqg_orthogonalize(ctx.h, ctypes.byref(u), ctypes.byref(o), ctypes.byref(p), _stream(stream)))
+
+
+def mqg_muon_step(ctx: Context, grad: torch.Tensor, momentum: torch.Tensor, weight: torch.Tensor, *, lr: float, beta: float = 0.95,
+                  nesterov: bool = True, weight_decay: float = 0.0, scale: Optional[float] = None, steps: int = 5, coeffs=None,
+                  eps: float = 1e-7, stream=None) -> None:
+    """momentum = beta momentum + grad; weight = (1 - lr weight_decay) weight - lr scale orthogonalize(grad + beta momentum, or momentum),
+    in place (float32).  scale: sqrt(max(1, rows / cols)) if none is given."""
+    assert grad.shape == momentum.shape == weight.shape
+    if scale is None:
+        scale = max(1.0, grad.shape[-2] / max(1, grad.shape[-1])) ** 0.5
+    g, m, w, p = _matrices(grad), _matrices(momentum), _matrices(weight), _orth(steps, coeffs, eps)
+    ctx.check(lib.mqg_muon_step(ctx.h, ctypes.byref(g), ctypes.byref(m), ctypes.byref(w), lr, beta, int(nesterov), weight_decay, scale,
+                                ctypes.byref(p), _stream(stream)))
 
 
 def mqg_queue_size(max_prepare_ms: float, mean_compute_ms: float, total_mem_bytes: int, peak_mem_bytes: int,
