@@ -13,9 +13,9 @@
 // product in 32 bits at a third of the f16 rate (which is five times the rate of the card's 32-bit matrix instructions).
 // Every matrix is stored times a power of two that puts the largest value it can have (known from the polynomial alone) just below f16's
 // largest, which leaves 2^-39 of it for the smallest.
-// Lines.  128 bytes of a row hold 32 values: their 32 high terms, then their 32 low ones.  A step of a product takes one line of every
-// row of its tile, from memory to LDS without registers between; the 16-byte chunks of row r change places by an exclusive or with
-// bits of r, so that the 16 rows that a wavefront reads together lie in different banks.
+// Blocks.  A matrix is stored as blocks of 32 rows by 32 values, 4 KB, in the order in which the matrix instruction takes them: the high
+// terms' four chunks of eight values, 32 rows each, then the low terms'.  Whatever reads an operand reads 1 KB that lies
+// together, from memory to LDS without registers between, from LDS without bank conflicts, or from memory to registers.
 #include <algorithm>
 #include <cmath>
 
@@ -27,16 +27,15 @@ namespace mqg {
 namespace {
 
 typedef F16 Half8 __attribute__((ext_vector_type(8)));
-typedef F16 Half4 __attribute__((ext_vector_type(4)));
+typedef float Float4 __attribute__((ext_vector_type(4)));
 typedef float Float16v __attribute__((ext_vector_type(16)));
 
-constexpr int kLine = 64;             // f16 of a line of 128 bytes
-constexpr int kLineVals = 32;         // values of a line
+constexpr int kSide = 32;             // rows and values of a block
+constexpr int kBlockLen = 2 * kSide * kSide;     // f16 of a block
+constexpr int kTermLen = kSide * kSide;
 
-__device__ __forceinline__ int chunk_place(int row, int chunk) { return chunk ^ (row & 7) ^ ((row >> 3) & 1); }
-
-// Position of value v of a row: its high term's; the low term's is kLineVals further.
-__device__ __forceinline__ int64_t term_at(int v) { return int64_t(v / kLineVals) * kLine + v % kLineVals; }
+// Chunk c (values 8 c to 8 c + 7) of row r of a block: its high terms'; the low ones are kTermLen further
+__device__ __forceinline__ int chunk_at(int r, int c) { return (c * kSide + r) * 8; }
 
 __device__ __forceinline__ void split(float v, F16 *hi, F16 *lo) {
     *hi = static_cast<F16>(v);
@@ -67,11 +66,10 @@ k_muon_momentum(UpdateArgs a) {
     float *mom = a.momentum ? a.momentum + mat * a.mom_mat : nullptr;
     constexpr int V = Vec<T>::kLen;
     double squares = 0.0;
-    const int vecs = (a.cols + V - 1) / V;
-    const int64_t all = int64_t(a.rows) * vecs;
-    for (int64_t t = int64_t(blockIdx.x) * kBlock + threadIdx.x; t < all; t += int64_t(gridDim.x) * kBlock) {
+    const uint32_t vecs = static_cast<uint32_t>(a.cols + V - 1) / V, all = static_cast<uint32_t>(a.rows) * vecs;       // 2^30 at most
+    for (uint32_t t = blockIdx.x * kBlock + threadIdx.x; t < all; t += gridDim.x * kBlock) {
         const int64_t r = t / vecs;
-        const int i = static_cast<int>(t - r * vecs);
+        const int i = static_cast<int>(t - static_cast<uint32_t>(r) * vecs);
         float g[V];
         load_vec(grad + r * a.grad_row, i, a.cols, g);
         if (mom) {
@@ -109,6 +107,21 @@ k_orth_split(UpdateArgs a, int num_parts, float unit, F16 *__restrict__ same, F1
     __shared__ float tile[kSplitTile][kSplitTile + 1];
     __shared__ double lds[kWavesPerBlock];
     const int mat = static_cast<int>(blockIdx.z);
+    const int r0 = static_cast<int>(blockIdx.y) * kSplitTile, c0 = static_cast<int>(blockIdx.x) * kSplitTile;
+    const T *grad = static_cast<const T *>(a.grad) + mat * a.grad_mat;
+    const float *mom = a.momentum ? a.momentum + mat * a.mom_mat : nullptr;
+    // the tile's values and the shares of the norm are on their way together
+    constexpr int kStep = kBlock / kSplitTile, kEach = kSplitTile / kStep;
+    const int c = static_cast<int>(threadIdx.x) % kSplitTile, first = static_cast<int>(threadIdx.x) / kSplitTile;
+    const bool col_in = c0 + c < a.cols;
+    float v[kEach], m[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int r = r0 + first + k * kStep;
+        const bool in = col_in && r < a.rows;
+        v[k] = in ? static_cast<float>(grad[int64_t(r) * a.grad_row + c0 + c]) : 0.f;
+        m[k] = in && mom ? mom[int64_t(r) * a.mom_row + c0 + c] : 0.f;
+    }
     double squares = 0.0;
     for (int p = static_cast<int>(threadIdx.x); p < num_parts; p += kBlock) squares += a.parts[int64_t(mat) * num_parts + p];
     for (int off = 32; off > 0; off >>= 1) squares += __shfl_xor(squares, off, kWave);
@@ -116,37 +129,28 @@ k_orth_split(UpdateArgs a, int num_parts, float unit, F16 *__restrict__ same, F1
     __syncthreads();
     const double norm = sqrt((lds[0] + lds[1]) + (lds[2] + lds[3]));
     const double inv = static_cast<double>(unit) / (norm + static_cast<double>(a.eps));
-    const int r0 = static_cast<int>(blockIdx.y) * kSplitTile, c0 = static_cast<int>(blockIdx.x) * kSplitTile;
-    const T *grad = static_cast<const T *>(a.grad) + mat * a.grad_mat;
-    const float *mom = a.momentum ? a.momentum + mat * a.mom_mat : nullptr;
-    const int c = static_cast<int>(threadIdx.x) % kSplitTile;
-    for (int r = static_cast<int>(threadIdx.x) / kSplitTile; r < kSplitTile; r += kBlock / kSplitTile) {
-        float v = 0.f;
-        if (r0 + r < a.rows && c0 + c < a.cols) {
-            const float g = static_cast<float>(grad[int64_t(r0 + r) * a.grad_row + c0 + c]);
-            v = static_cast<float>(update_of(a, g, mom ? mom[int64_t(r0 + r) * a.mom_row + c0 + c] : 0.f) * inv);
-        }
-        tile[r][c] = v;
-    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) tile[first + k * kStep][c] = static_cast<float>(update_of(a, v[k], m[k]) * inv);
     __syncthreads();
     const int64_t mat_len = int64_t(pad_rows) * pad_cols * 2;
-    for (int side = 0; side < 2; ++side) {
+    for (int side = 0; side < 2; ++side) {                 // 2 x 2 blocks each way, 128 threads to a block
         F16 *base = (side ? turned : same) + mat * mat_len;
-        const int row0 = side ? c0 : r0, val0 = side ? r0 : c0, len = side ? pad_rows : pad_cols;
-        const int row = static_cast<int>(threadIdx.x) / 4, part = static_cast<int>(threadIdx.x) % 4 * 16;      // 16 values of a row
-        F16 *to = base + (row0 + row) * (int64_t(len) * 2) + term_at(val0 + part);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        const int row0 = (side ? c0 : r0) / kSide, val0 = (side ? r0 : c0) / kSide, blocks = (side ? pad_rows : pad_cols) / kSide;
+        const int row = static_cast<int>(threadIdx.x) % kSide, chunk = static_cast<int>(threadIdx.x) / kSide % 4;
+        for (int k = static_cast<int>(threadIdx.x) / 128; k < 4; k += 2) {
+            const int rb = k / 2, vb = k % 2;
             Half8 hi, lo;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
+                const int r = rb * kSide + row, v = vb * kSide + chunk * 8 + j;
                 F16 x, y;
-                split(side ? tile[part + 8 * h + j][row] : tile[row][part + 8 * h + j], &x, &y);
+                split(side ? tile[v][r] : tile[r][v], &x, &y);
                 hi[j] = x;
                 lo[j] = y;
             }
-            *reinterpret_cast<Half8 *>(to + 8 * h) = hi;
-            *reinterpret_cast<Half8 *>(to + kLineVals + 8 * h) = lo;
+            F16 *to = base + (int64_t(row0 + rb) * blocks + val0 + vb) * kBlockLen + chunk_at(row, chunk);
+            *reinterpret_cast<Half8 *>(to) = hi;
+            *reinterpret_cast<Half8 *>(to + kTermLen) = lo;
         }
     }
 }
@@ -156,16 +160,17 @@ k_orth_split(UpdateArgs a, int num_parts, float unit, F16 *__restrict__ same, F1
 enum Epilogue { kGram, kPoly, kIterate, kOut };
 
 struct ProductArgs {
-    const F16 *p, *q;                 // P [m x depth], Q [n x depth], in lines
-    const F16 *own;                   // [m x n] what the epilogue adds `own_by` times
+    const F16 *p, *q;                 // P [m x depth], Q [n x depth]
+    const F16 *own;                   // [m x n]: what the epilogue adds `own_by` times
     F16 *to, *to_turned;              // [m x n], [n x m]
-    int64_t p_mat, q_mat, own_mat, to_mat, turned_mat;     // f16 from a matrix of the stack to the next
-    int32_t depth;                    // values of a row, a multiple of kLineVals
+    int64_t p_mat, q_mat, own_mat, to_mat;     // f16 from a matrix of the stack to the next (to_turned: as to)
+    int32_t depth;                    // values of a row
     int32_t m, n;                     // padded, multiples of the tile
-    int32_t tiles_m, tiles_n;
+    int32_t tiles_m, tiles_n, tiles;  // tiles: of a matrix
+    int32_t first_tile;
     float acc_by, own_by;
     // the last product
-    void *out;                        // update wanted: [m x n] of out_type; or the weights
+    void *out;                        // [m x n] of out_type, or the weights
     int64_t out_row, out_mat;
     int32_t out_m, out_n;             // unpadded
     int32_t out_type;                 // mqg_dtype
@@ -173,40 +178,161 @@ struct ProductArgs {
     float keep;
 };
 
-// out = acc_by (P Q^T) + own_by own, tiles of (WM FM 32) x (WN FN 32) by WM x WN wavefronts.
+// Which matrix and tile a workgroup takes.  Workgroups go to the chip's eight dies in turn, each with an L2 of its own: a die gets a run of
+// neighbouring tiles, bands of kBand rows of tiles taken column by column, so that the tiles that it works on together share rows and columns.
+constexpr int kDies = 8, kBand = 8;
+struct TilePlace {
+    int mat, m, n;
+};
+__device__ __forceinline__ int dealt_tile() {
+    const int all = static_cast<int>(gridDim.x), id = static_cast<int>(blockIdx.x);
+    const int die = id % kDies, more = all % kDies;
+    return die * (all / kDies) + (die < more ? die : more) + id / kDies;
+}
+template <bool SYMMETRIC>
+__device__ __forceinline__ TilePlace tile_place(const ProductArgs &a, int at) {
+    TilePlace t;
+    t.mat = at / a.tiles;
+    int i = at - t.mat * a.tiles;
+    if constexpr (SYMMETRIC) {                             // the tiles on and below the diagonal: band b has 8 rows of 8 b tiles and a triangle of 36
+        int b = static_cast<int>((sqrtf(8.f * static_cast<float>(i) + 1.f) - 1.f) * 0.5f) / kBand;
+        while (4 * b * (kBand * b + 1) > i) --b;
+        while (4 * (b + 1) * (kBand * (b + 1) + 1) <= i) ++b;
+        i -= 4 * b * (kBand * b + 1);
+        const int rows = a.tiles_m - b * kBand < kBand ? a.tiles_m - b * kBand : kBand;
+        if (i < rows * kBand * b) {
+            t.n = i / rows;
+            t.m = b * kBand + i - t.n * rows;
+        } else {
+            i -= rows * kBand * b;
+            int r = 0;
+            while (i > r) i -= ++r;
+            t.m = b * kBand + r;
+            t.n = b * kBand + i;
+        }
+    } else {
+        const int b = i / (kBand * a.tiles_n);
+        i -= b * kBand * a.tiles_n;
+        const int rows = a.tiles_m - b * kBand < kBand ? a.tiles_m - b * kBand : kBand;
+        t.n = i / rows;
+        t.m = b * kBand + i - t.n * rows;
+    }
+    return t;
+}
+static_assert(kBand == 8, "the counts of tiles before a band are written out");
+
+// The epilogue of one block of the product, 32 x 32, whose sums lie in LDS as the matrix instruction leaves them, register e of lane l at
+// e * kAccRow + l: row 8 (e / 4) + 4 (l / 32) + e % 4, column l % 32.  PARTS of them, part_len apart, are added; the finished values go back to the
+// first, from which they are stored turned.  `threads` threads, t among them; sync() orders LDS between them.
+constexpr int kAccRow = kWave + 4;    // (16 rows of a column in other banks)
+constexpr int kAccLen = 16 * kAccRow;
+template <int EPI, int PARTS, typename Sync>
+__device__ __forceinline__ void finish_block(const ProductArgs &a, float *acc, int part_len, int mat, int mb, int nb, bool mirror, int t, int threads, Sync sync) {
+    auto store = [&](const float (&v)[8], F16 *to) __attribute__((always_inline)) {
+        Half8 hi, lo;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            F16 x, y;
+            split(v[j], &x, &y);
+            hi[j] = x;
+            lo[j] = y;
+        }
+        *reinterpret_cast<Half8 *>(to) = hi;
+        *reinterpret_cast<Half8 *>(to + kTermLen) = lo;
+    };
+    const int64_t block = (int64_t(mb) * (a.n / kSide) + nb) * kBlockLen, block_turned = (int64_t(nb) * (a.m / kSide) + mb) * kBlockLen;
+    for (int u = t; u < 128; u += threads) {               // eight columns of a row; the output is written along its rows, four threads to each
+        const int r = EPI == kOut ? u >> 2 : u % kSide, c = EPI == kOut ? u & 3 : u / kSide;
+        float *at = acc + ((r >> 3) * 4 + (r & 3)) * kAccRow + 32 * ((r >> 2) & 1) + 8 * c;
+        Half8 own_hi, own_lo;
+        if constexpr (EPI != kGram) {
+            const F16 *own = a.own + mat * a.own_mat + block + chunk_at(r, c);
+            own_hi = *reinterpret_cast<const Half8 *>(own);
+            own_lo = *reinterpret_cast<const Half8 *>(own + kTermLen);
+        }
+        Float4 x{0, 0, 0, 0}, y{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+            x += *reinterpret_cast<const Float4 *>(at + k * part_len);
+            y += *reinterpret_cast<const Float4 *>(at + k * part_len + 4);
+        }
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = (j < 4 ? x[j % 4] : y[j % 4]) * a.acc_by;
+            if constexpr (EPI != kGram) v[j] += a.own_by * (static_cast<float>(own_hi[j]) + static_cast<float>(own_lo[j]));
+        }
+        if constexpr (EPI != kOut) {
+            store(v, a.to + mat * a.to_mat + block + chunk_at(r, c));
+            if (EPI == kIterate || mirror) {
+                *reinterpret_cast<Float4 *>(at) = Float4{v[0], v[1], v[2], v[3]};
+                *reinterpret_cast<Float4 *>(at + 4) = Float4{v[4], v[5], v[6], v[7]};
+            }
+        } else {
+            const int row = mb * kSide + r, col0 = nb * kSide + 8 * c;
+            if (row >= a.out_m) continue;
+            const int64_t to = mat * a.out_mat + row * a.out_row;
+            if (a.step) {
+                float *w = static_cast<float *>(a.out) + to;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (col0 + 4 * h >= a.out_n) continue;
+                    float z[4];
+                    load_vec(w, col0 / 4 + h, a.out_n, z);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) z[j] = a.keep * z[j] + v[4 * h + j];
+                    store_vec(w, col0 / 4 + h, a.out_n, z);
+                }
+            } else if (a.out_type == MQG_F16) {
+                store_vec(static_cast<F16 *>(a.out) + to, col0 / 8, a.out_n, v);
+            } else if (a.out_type == MQG_BF16) {
+                store_vec(static_cast<BF16 *>(a.out) + to, col0 / 8, a.out_n, v);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float z[4] = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+                    store_vec(static_cast<float *>(a.out) + to, col0 / 4 + h, a.out_n, z);
+                }
+            }
+        }
+    }
+    if constexpr (EPI != kOut) {
+        if (EPI != kIterate && !mirror) return;            // (the same in all threads of a tile)
+        sync();
+        for (int u = t; u < 128; u += threads) {           // eight rows of a column
+            const int col = u % kSide, c = u / kSide;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = acc[(c * 4 + (j & 3)) * kAccRow + col + 32 * (j >> 2)];
+            store(v, a.to_turned + mat * a.to_mat + block_turned + chunk_at(col, c));
+        }
+    }
+}
+
+// out = acc_by (P Q^T) + own_by own, tiles of (WM FM 32) x (WN FN 32) by WM x WN wavefronts, blocks through LDS, the next
+// blocks on their way while these are multiplied.
 template <int EPI, int WM, int WN, int FM, int FN>
 __global__ void __launch_bounds__(WM * WN * kWave)
 k_orth_product(ProductArgs a) {
-    constexpr int BM = WM * FM * 32, BN = WN * FN * 32, kWaves = WM * WN;
-    constexpr int kStage = (BM + BN) * kLine;
-    __shared__ F16 lds[2 * kStage];
+    constexpr int BM = WM * FM, BN = WN * FN, kWaves = WM * WN;            // the tile in blocks
+    constexpr int kStage = (BM + BN) * kBlockLen;
+    static_assert(kWaves * kAccLen * sizeof(float) <= 2 * kStage * sizeof(F16), "the epilogue's blocks fit");
+    __shared__ __attribute__((aligned(16))) F16 lds[2 * kStage];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    const int mat = static_cast<int>(blockIdx.y);
-    int tm, tn;
-    if constexpr (EPI == kGram || EPI == kPoly) {          // symmetric: the tiles on and below the diagonal
-        const int t = static_cast<int>(blockIdx.x);
-        tm = static_cast<int>((sqrtf(8.f * static_cast<float>(t) + 1.f) - 1.f) * 0.5f);
-        while (tm * (tm + 1) / 2 > t) --tm;
-        while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
-        tn = t - tm * (tm + 1) / 2;
-    } else {
-        tm = static_cast<int>(blockIdx.x) / a.tiles_n;
-        tn = static_cast<int>(blockIdx.x) - tm * a.tiles_n;
-    }
-    const int64_t row_len = int64_t(a.depth) * 2;
-    const F16 *p = a.p + mat * a.p_mat + int64_t(tm) * BM * row_len;
-    const F16 *q = a.q + mat * a.q_mat + int64_t(tn) * BN * row_len;
+    const TilePlace tile = tile_place<EPI == kGram || EPI == kPoly>(a, dealt_tile());
+    const int deep = a.depth / kSide;
+    const F16 *p = a.p + tile.mat * a.p_mat + int64_t(tile.m) * BM * deep * kBlockLen;
+    const F16 *q = a.q + tile.mat * a.q_mat + int64_t(tile.n) * BN * deep * kBlockLen;
 
-    // one line of each of the tile's rows: eight rows per instruction of a wavefront, lane l has place l % 8 of row l / 8
+    // blocks number `line` of the tile's rows of blocks, four instructions of a wavefront each
     auto fetch = [&](int line, int stage) __attribute__((always_inline)) {
         F16 *to = lds + stage * kStage;
 #pragma unroll
-        for (int r = 0; r < (BM + BN) / 8; r += kWaves) {
-            const int row = (r + wave) * 8 + (lane >> 3);
-            const int chunk = chunk_place(row, lane & 7);  // (an exclusive or: its own inverse)
-            const F16 *from = (row < BM ? p + row * row_len : q + (row - BM) * row_len) + int64_t(line) * kLine + chunk * 8;
+        for (int u = 0; u < (BM + BN) * 4; u += kWaves) {
+            const int unit = u + wave, b = unit / 4;
+            const F16 *from = (b < BM ? p + int64_t(b) * deep * kBlockLen : q + int64_t(b - BM) * deep * kBlockLen) + int64_t(line) * kBlockLen + (unit % 4) * 512 + lane * 8;
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                             (__attribute__((address_space(3))) void *)(to + (r + wave) * 8 * kLine), 16, 0, 0);
+                                             (__attribute__((address_space(3))) void *)(to + unit * 512), 16, 0, 0);
         }
     };
     Float16v acc[FM][FN];
@@ -214,32 +340,27 @@ k_orth_product(ProductArgs a) {
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = Float16v{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-    const int wm = wave / WN * FM * 32, wn = wave % WN * FN * 32;
-    const int lines = a.depth / kLineVals;
+    const int wm = wave / WN * FM, wn = wave % WN * FN;
     fetch(0, 0);
-    for (int line = 0; line < lines; ++line) {
+    for (int line = 0; line < deep; ++line) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the line has arrived,
         __syncthreads();                                   // in every wavefront, and the other stage has been read
-        if (line + 1 < lines) fetch(line + 1, (line + 1) & 1);
-        const F16 *at = lds + (line & 1) * kStage;
+        if (line + 1 < deep) fetch(line + 1, (line + 1) & 1);
+        const F16 *at = lds + (line & 1) * kStage + lane * 8;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {                      // 16 values at a time
             Half8 ph[FM], pl[FM], qh[FN], ql[FN];
-            auto read = [&](int row, int chunk) __attribute__((always_inline)) {
-                return *reinterpret_cast<const Half8 *>(at + row * kLine + chunk_place(row, chunk) * 8);
-            };
-            const int c = 2 * t + (lane >> 5);
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                const int row = wm + i * 32 + (lane & 31);
-                ph[i] = read(row, c);
-                pl[i] = read(row, c + 4);
+                const F16 *b = at + (wm + i) * kBlockLen + t * 512;
+                ph[i] = *reinterpret_cast<const Half8 *>(b);
+                pl[i] = *reinterpret_cast<const Half8 *>(b + kTermLen);
             }
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                const int row = BM + wn + j * 32 + (lane & 31);
-                qh[j] = read(row, c);
-                ql[j] = read(row, c + 4);
+                const F16 *b = at + (BM + wn + j) * kBlockLen + t * 512;
+                qh[j] = *reinterpret_cast<const Half8 *>(b);
+                ql[j] = *reinterpret_cast<const Half8 *>(b + kTermLen);
             }
 #pragma unroll
             for (int i = 0; i < FM; ++i)
@@ -251,61 +372,72 @@ k_orth_product(ProductArgs a) {
                 }
         }
     }
-
-    // register e of lane l: row 8 (e / 4) + 4 (l / 32) + e % 4, column l % 32
-    const F16 *own = EPI == kGram ? nullptr : a.own + mat * a.own_mat;
+    __syncthreads();                                       // the stages are free
+    float *mine = reinterpret_cast<float *>(lds) + wave * kAccLen;
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int j = 0; j < FN; ++j) {
 #pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-                const int row = tm * BM + wm + i * 32 + 8 * e4 + 4 * (lane >> 5);      // of four
-                const int col = tn * BN + wn + j * 32 + (lane & 31);
-                float v[4];
-                Half4 hi4, lo4;
+            for (int e = 0; e < 16; ++e) mine[e * kAccRow + lane] = acc[i][j][e];
+            wave_lds_sync();
+            finish_block<EPI, 1>(a, mine, 0, tile.mat, tile.m * BM + wm + i, tile.n * BN + wn + j, tile.m != tile.n, lane, kWave, [] { wave_lds_sync(); });
+            wave_lds_sync();
+        }
+}
+
+// The same for few tiles: a block of the product to a workgroup, whose depth eight wavefronts share.  Each takes every eighth block of P and
+// of Q, from memory to registers, up to kAhead of them on their way together, and the eight sums are added in LDS.
+// SUB > 1: the blocks of the tiles of SUB x SUB blocks from number first_tile on.
+constexpr int kFewWaves = 8;
+template <int EPI, int SUB>
+__global__ void __launch_bounds__(kFewWaves * kWave) __attribute__((amdgpu_waves_per_eu(4, 4)))
+k_orth_product_few(ProductArgs a) {
+    constexpr bool symmetric = EPI == kGram || EPI == kPoly;
+    constexpr int kAhead = 3;
+    __shared__ __attribute__((aligned(16))) float lds[kFewWaves * kAccLen];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    TilePlace tile = tile_place<symmetric>(a, SUB == 1 ? dealt_tile() : a.first_tile + static_cast<int>(blockIdx.x) / (SUB * SUB));
+    const bool mirror = tile.m != tile.n;
+    if constexpr (SUB > 1) {
+        const int sub = static_cast<int>(blockIdx.x) % (SUB * SUB);
+        tile.m = tile.m * SUB + sub / SUB;
+        tile.n = tile.n * SUB + sub % SUB;
+    }
+    const int deep = a.depth / kSide;
+    const F16 *p = a.p + tile.mat * a.p_mat + int64_t(tile.m) * deep * kBlockLen + lane * 8;
+    const F16 *q = a.q + tile.mat * a.q_mat + int64_t(tile.n) * deep * kBlockLen + lane * 8;
+    Float16v acc = Float16v{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    // N blocks from number `line` on: all their loads, then their products
+    auto batch = [&](int line, auto number) __attribute__((always_inline)) {
+        constexpr int N = decltype(number)::value;
+        Half8 pv[N][4], qv[N][4];                          // high terms of the block's halves, low terms
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = acc[i][j][4 * e4 + e] * a.acc_by;
-                    if constexpr (EPI != kGram) {
-                        const F16 *o = own + (row + e) * (int64_t(a.n) * 2) + term_at(col);
-                        v[e] += a.own_by * (static_cast<float>(o[0]) + static_cast<float>(o[kLineVals]));
-                    }
-                    F16 hi, lo;
-                    split(v[e], &hi, &lo);
-                    hi4[e] = hi;
-                    lo4[e] = lo;
-                }
-                if constexpr (EPI == kOut) {
+        for (int u = 0; u < N; ++u)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (row + e >= a.out_m || col >= a.out_n) continue;
-                        const int64_t at = mat * a.out_mat + (row + e) * a.out_row + col;
-                        if (a.step) {
-                            float *w = static_cast<float *>(a.out) + at;
-                            *w = a.keep * *w + v[e];
-                        } else if (a.out_type == MQG_F16) {
-                            static_cast<F16 *>(a.out)[at] = static_cast<F16>(v[e]);
-                        } else if (a.out_type == MQG_BF16) {
-                            static_cast<BF16 *>(a.out)[at] = static_cast<BF16>(v[e]);
-                        } else {
-                            static_cast<float *>(a.out)[at] = v[e];
-                        }
-                    }
-                } else {
-                    F16 *to = a.to + mat * a.to_mat + row * (int64_t(a.n) * 2) + term_at(col);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        to[e * (int64_t(a.n) * 2)] = hi4[e];
-                        to[e * (int64_t(a.n) * 2) + kLineVals] = lo4[e];
-                    }
-                    if (EPI == kIterate || tm != tn) {
-                        F16 *turned = (EPI == kIterate ? a.to_turned + mat * a.turned_mat : a.to + mat * a.to_mat) + col * (int64_t(a.m) * 2) + term_at(row);
-                        *reinterpret_cast<Half4 *>(turned) = hi4;
-                        *reinterpret_cast<Half4 *>(turned + kLineVals) = lo4;
-                    }
-                }
+            for (int k = 0; k < 4; ++k) {
+                pv[u][k] = *reinterpret_cast<const Half8 *>(p + int64_t(line + u * kFewWaves) * kBlockLen + k * 512);
+                qv[u][k] = *reinterpret_cast<const Half8 *>(q + int64_t(line + u * kFewWaves) * kBlockLen + k * 512);
             }
+        __builtin_amdgcn_sched_barrier(0);                 // (the compiler would put every load where it is used, one after the other)
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[u][t], qv[u][2 + t], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[u][2 + t], qv[u][t], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[u][t], qv[u][t], acc, 0, 0, 0);
+            }
+    };
+    using std::integral_constant;
+    int line = wave, left = (deep - wave + kFewWaves - 1) / kFewWaves;
+    for (; left >= kAhead; left -= kAhead, line += kAhead * kFewWaves) batch(line, integral_constant<int, kAhead>());
+    if (left == 2) batch(line, integral_constant<int, 2>());
+    if (left == 1) batch(line, integral_constant<int, 1>());
+#pragma unroll
+    for (int e = 0; e < 16; ++e) lds[wave * kAccLen + e * kAccRow + lane] = acc[e];
+    __syncthreads();
+    finish_block<EPI, kFewWaves>(a, lds, kAccLen, tile.mat, tile.m, tile.n, mirror, static_cast<int>(threadIdx.x), kFewWaves * kWave, [] { __syncthreads(); });
 }
 
 // ---------------------------------------------------------------- host side
@@ -345,8 +477,9 @@ int unit_exp(double most) {
     return 15 - e;
 }
 
-constexpr int kOrthTile = 128;
-constexpr int kOrthParts = 256;       // workgroups per matrix that share its norm
+constexpr int kFewSide = 512;          // smaller sides up to this: see launch_product
+constexpr int kOrthTile = 128, kOrthPad = kSplitTile;
+constexpr int kOrthParts = 1024;      // workgroups per matrix that share its norm
 
 struct OrthLayout {
     int64_t n, k;                     // padded
@@ -355,8 +488,10 @@ struct OrthLayout {
 };
 OrthLayout orth_layout(int64_t mats, int64_t rows, int64_t cols) {
     OrthLayout l;
-    l.n = ceil_div(std::min(rows, cols), kOrthTile) * kOrthTile;
-    l.k = ceil_div(std::max(rows, cols), kOrthTile) * kOrthTile;
+    const int64_t n = std::min(rows, cols), k = std::max(rows, cols);
+    const int64_t pad = n > kFewSide ? kOrthTile : kOrthPad;
+    l.n = ceil_div(n, pad) * pad;
+    l.k = ceil_div(k, pad) * pad;
     l.x = l.n * l.k * 2;
     l.g = l.n * l.n * 2;
     l.parts = ceil_div(mats * kOrthParts * int64_t(sizeof(double)), 256) * 256;
@@ -364,14 +499,31 @@ OrthLayout orth_layout(int64_t mats, int64_t rows, int64_t cols) {
     return l;
 }
 
+// Two tiles of 128 x 128 fit a compute unit.  A few tiles more than whole rounds of the chip would take as long as a round; up to kTileRest of
+// them go block by block, their depth shared by the wavefronts.
+constexpr int kTileRound = 512, kTileRest = 64;
 template <int EPI>
-int launch_product(mqg_ctx *ctx, ProductArgs a, int64_t mats, hipStream_t s) {
+int launch_product(mqg_ctx *ctx, ProductArgs a, int64_t mats, bool few, hipStream_t s) {
     static const char *const names[] = {"k_orth_gram", "k_orth_poly", "k_orth_iterate", "k_orth_out"};
-    a.tiles_m = a.m / kOrthTile;
-    a.tiles_n = a.n / kOrthTile;
-    const int64_t tiles = EPI == kGram || EPI == kPoly ? int64_t(a.tiles_m) * (a.tiles_m + 1) / 2 : int64_t(a.tiles_m) * a.tiles_n;
-    const dim3 grid(static_cast<uint32_t>(tiles), static_cast<uint32_t>(mats));
-    MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product<EPI, 2, 2, 2, 2><<<grid, 256, 0, s>>>(a)));
+    constexpr bool symmetric = EPI == kGram || EPI == kPoly;
+    auto tiles_of = [&](int side) {
+        a.tiles_m = a.m / side;
+        a.tiles_n = a.n / side;
+        a.tiles = symmetric ? static_cast<int32_t>(int64_t(a.tiles_m) * (a.tiles_m + 1) / 2) : a.tiles_m * a.tiles_n;
+        return int64_t(a.tiles) * mats;
+    };
+    if (few) {
+        const int grid = static_cast<int>(tiles_of(kSide));
+        MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product_few<EPI, 1><<<grid, kFewWaves * kWave, 0, s>>>(a)));
+        return MQG_OK;
+    }
+    const int all = static_cast<int>(tiles_of(kOrthTile)), rest = all > kTileRound && all % kTileRound <= kTileRest ? all % kTileRound : 0;
+    MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product<EPI, 2, 2, 2, 2><<<all - rest, 256, 0, s>>>(a)));
+    if (rest) {
+        constexpr int sub = kOrthTile / kSide;
+        a.first_tile = all - rest;
+        MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product_few<EPI, sub><<<rest * sub * sub, kFewWaves * kWave, 0, s>>>(a)));
+    }
     return MQG_OK;
 }
 
@@ -401,7 +553,7 @@ int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
     F16 *x = reinterpret_cast<F16 *>(ctx->layer_scratch + l.parts);          // X: n rows of k values
     F16 *xt[2] = {x + mats * l.x, x + 2 * mats * l.x};                       // its transpose, in turns
     F16 *gram = x + 3 * mats * l.x, *poly = gram + mats * l.g;
-    const bool tall = rows > cols;
+    const bool tall = rows > cols, few = std::min(rows, cols) <= kFewSide;
 
     UpdateArgs u{call.grad, call.momentum, call.grad_row, call.grad_mat, call.mom_row, call.mom_mat, parts, static_cast<int32_t>(rows),
                  static_cast<int32_t>(cols), call.nesterov, call.beta, call.eps};
@@ -432,19 +584,19 @@ int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
         a.p_mat = a.q_mat = l.x;
         a.depth = static_cast<int32_t>(l.k);
         a.m = a.n = static_cast<int32_t>(l.n);
-        a.to = gram;
+        a.to = a.to_turned = gram;
         a.to_mat = l.g;
         a.acc_by = std::ldexp(1.f, eg - 2 * ex);
-        rc = launch_product<kGram>(ctx, a, mats, s);
+        rc = launch_product<kGram>(ctx, a, mats, few, s);
         if (rc != MQG_OK) return rc;
 
         a.p = a.q = a.own = gram;
         a.p_mat = a.q_mat = a.own_mat = l.g;
         a.depth = static_cast<int32_t>(l.n);
-        a.to = poly;
+        a.to = a.to_turned = poly;
         a.acc_by = k[2] * std::ldexp(1.f, eb - 2 * eg);
         a.own_by = k[1] * std::ldexp(1.f, eb - eg);
-        rc = launch_product<kPoly>(ctx, a, mats, s);
+        rc = launch_product<kPoly>(ctx, a, mats, few, s);
         if (rc != MQG_OK) return rc;
 
         r = poly_most(k, r) * 1.001;
@@ -460,13 +612,13 @@ int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
         a.q = tall ? poly : now;
         a.q_mat = tall ? l.g : l.x;
         a.own = tall ? now : x;
-        a.own_mat = a.to_mat = a.turned_mat = l.x;
+        a.own_mat = a.to_mat = l.x;
         a.to = tall ? then : x;
         a.to_turned = tall ? x : then;
         a.m = static_cast<int32_t>(tall ? l.k : l.n);
         a.n = static_cast<int32_t>(tall ? l.n : l.k);
         if (!last) {
-            rc = launch_product<kIterate>(ctx, a, mats, s);
+            rc = launch_product<kIterate>(ctx, a, mats, few, s);
         } else {
             a.out = call.out;
             a.out_row = call.out_row;
@@ -476,7 +628,7 @@ int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
             a.out_type = call.out_type;
             a.step = call.step;
             a.keep = call.keep;
-            rc = launch_product<kOut>(ctx, a, mats, s);
+            rc = launch_product<kOut>(ctx, a, mats, few, s);
         }
         if (rc != MQG_OK) return rc;
         ex = next;
