@@ -27,6 +27,7 @@ namespace mqg {
 namespace {
 
 typedef F16 Half8 __attribute__((ext_vector_type(8)));
+typedef F16 Half4 __attribute__((ext_vector_type(4)));
 typedef float Float4 __attribute__((ext_vector_type(4)));
 typedef float Float16v __attribute__((ext_vector_type(16)));
 
@@ -309,13 +310,13 @@ __device__ __forceinline__ void finish_block(const ProductArgs &a, float *acc, i
     }
 }
 
-// out = acc_by (P Q^T) + own_by own, tiles of (WM FM 32) x (WN FN 32) by WM x WN wavefronts, blocks through LDS, the next
-// blocks on their way while these are multiplied.
+// out = acc_by (P Q^T) + own_by own, tiles of (WM FM 32) x (WN FN 32) by WM x WN wavefronts, blocks through LDS, the
+// next ones on their way while these are multiplied.
 template <int EPI, int WM, int WN, int FM, int FN>
 __global__ void __launch_bounds__(WM * WN * kWave)
 k_orth_product(ProductArgs a) {
     constexpr int BM = WM * FM, BN = WN * FN, kWaves = WM * WN;            // the tile in blocks
-    constexpr int kStage = (BM + BN) * kBlockLen;
+    constexpr int kStage = (BM + BN) * kBlockLen, kLoads = (BM + BN) * 4 / kWaves;      // of a wavefront
     static_assert(kWaves * kAccLen * sizeof(float) <= 2 * kStage * sizeof(F16), "the epilogue's blocks fit");
     __shared__ __attribute__((aligned(16))) F16 lds[2 * kStage];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
@@ -324,13 +325,14 @@ k_orth_product(ProductArgs a) {
     const F16 *p = a.p + tile.mat * a.p_mat + int64_t(tile.m) * BM * deep * kBlockLen;
     const F16 *q = a.q + tile.mat * a.q_mat + int64_t(tile.n) * BN * deep * kBlockLen;
 
-    // blocks number `line` of the tile's rows of blocks, four instructions of a wavefront each
+    // blocks number `line` of the tile's rows of blocks, 1 KB an instruction of a wavefront
     auto fetch = [&](int line, int stage) __attribute__((always_inline)) {
         F16 *to = lds + stage * kStage;
+        const int64_t at = int64_t(line) * kBlockLen + lane * 8;
 #pragma unroll
-        for (int u = 0; u < (BM + BN) * 4; u += kWaves) {
-            const int unit = u + wave, b = unit / 4;
-            const F16 *from = (b < BM ? p + int64_t(b) * deep * kBlockLen : q + int64_t(b - BM) * deep * kBlockLen) + int64_t(line) * kBlockLen + (unit % 4) * 512 + lane * 8;
+        for (int u = 0; u < kLoads; ++u) {
+            const int unit = u * kWaves + wave, b = unit / 4;
+            const F16 *from = (b < BM ? p + int64_t(b) * deep * kBlockLen : q + int64_t(b - BM) * deep * kBlockLen) + (unit % 4) * 512 + at;
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
                                              (__attribute__((address_space(3))) void *)(to + unit * 512), 16, 0, 0);
         }
@@ -343,8 +345,8 @@ k_orth_product(ProductArgs a) {
     const int wm = wave / WN * FM, wn = wave % WN * FN;
     fetch(0, 0);
     for (int line = 0; line < deep; ++line) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the line has arrived,
-        __syncthreads();                                   // in every wavefront, and the other stage has been read
+        // the line has arrived and this wavefront's reads of the other stage are done; behind the barrier that holds for all
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (line + 1 < deep) fetch(line + 1, (line + 1) & 1);
         const F16 *at = lds + (line & 1) * kStage + lane * 8;
 #pragma unroll
@@ -372,7 +374,7 @@ k_orth_product(ProductArgs a) {
                 }
         }
     }
-    __syncthreads();                                       // the stages are free
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");     // the stages are free
     float *mine = reinterpret_cast<float *>(lds) + wave * kAccLen;
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -386,16 +388,16 @@ k_orth_product(ProductArgs a) {
         }
 }
 
-// The same for few tiles: a block of the product to a workgroup, whose depth eight wavefronts share.  Each takes every eighth block of P and
-// of Q, from memory to registers, up to kAhead of them on their way together, and the eight sums are added in LDS.
+// The same for few tiles: F x F blocks of the product to a workgroup, whose depth eight wavefronts share.  Each takes every eighth block of P
+// and of Q, from memory to registers, AHEAD of them on their way together, and the eight sums are added in LDS.
 // SUB > 1: the blocks of the tiles of SUB x SUB blocks from number first_tile on.
 constexpr int kFewWaves = 8;
-template <int EPI, int SUB>
-__global__ void __launch_bounds__(kFewWaves * kWave) __attribute__((amdgpu_waves_per_eu(4, 4)))
+template <int EPI, int SUB, int F, int AHEAD>
+__global__ void __launch_bounds__(kFewWaves * kWave) __attribute__((amdgpu_waves_per_eu(F == 1 ? 4 : 2, F == 1 ? 4 : 2)))
 k_orth_product_few(ProductArgs a) {
     constexpr bool symmetric = EPI == kGram || EPI == kPoly;
-    constexpr int kAhead = 3;
-    __shared__ __attribute__((aligned(16))) float lds[kFewWaves * kAccLen];
+    static_assert(SUB == 1 || F == 1, "");
+    __shared__ __attribute__((aligned(16))) float lds[kFewWaves * F * F * kAccLen];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     TilePlace tile = tile_place<symmetric>(a, SUB == 1 ? dealt_tile() : a.first_tile + static_cast<int>(blockIdx.x) / (SUB * SUB));
     const bool mirror = tile.m != tile.n;
@@ -405,39 +407,336 @@ k_orth_product_few(ProductArgs a) {
         tile.n = tile.n * SUB + sub % SUB;
     }
     const int deep = a.depth / kSide;
-    const F16 *p = a.p + tile.mat * a.p_mat + int64_t(tile.m) * deep * kBlockLen + lane * 8;
-    const F16 *q = a.q + tile.mat * a.q_mat + int64_t(tile.n) * deep * kBlockLen + lane * 8;
-    Float16v acc = Float16v{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    const F16 *p = a.p + tile.mat * a.p_mat + int64_t(tile.m) * F * deep * kBlockLen + lane * 8;
+    const F16 *q = a.q + tile.mat * a.q_mat + int64_t(tile.n) * F * deep * kBlockLen + lane * 8;
+    Float16v acc[F][F];
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j) acc[i][j] = Float16v{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     // N blocks from number `line` on: all their loads, then their products
     auto batch = [&](int line, auto number) __attribute__((always_inline)) {
         constexpr int N = decltype(number)::value;
-        Half8 pv[N][4], qv[N][4];                          // high terms of the block's halves, low terms
+        Half8 pv[N][F][4], qv[N][F][4];                    // high terms of the block's halves, low terms
 #pragma unroll
         for (int u = 0; u < N; ++u)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                pv[u][k] = *reinterpret_cast<const Half8 *>(p + int64_t(line + u * kFewWaves) * kBlockLen + k * 512);
-                qv[u][k] = *reinterpret_cast<const Half8 *>(q + int64_t(line + u * kFewWaves) * kBlockLen + k * 512);
-            }
+            for (int i = 0; i < F; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int64_t at = (int64_t(i) * deep + line + u * kFewWaves) * kBlockLen + k * 512;
+                    pv[u][i][k] = *reinterpret_cast<const Half8 *>(p + at);
+                    qv[u][i][k] = *reinterpret_cast<const Half8 *>(q + at);
+                }
         __builtin_amdgcn_sched_barrier(0);                 // (the compiler would put every load where it is used, one after the other)
 #pragma unroll
         for (int u = 0; u < N; ++u)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[u][t], qv[u][2 + t], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[u][2 + t], qv[u][t], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[u][t], qv[u][t], acc, 0, 0, 0);
-            }
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < F; ++i)
+#pragma unroll
+                    for (int j = 0; j < F; ++j) {
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[u][i][t], qv[u][j][2 + t], acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[u][i][2 + t], qv[u][j][t], acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pv[u][i][t], qv[u][j][t], acc[i][j], 0, 0, 0);
+                    }
     };
     using std::integral_constant;
     int line = wave, left = (deep - wave + kFewWaves - 1) / kFewWaves;
-    for (; left >= kAhead; left -= kAhead, line += kAhead * kFewWaves) batch(line, integral_constant<int, kAhead>());
-    if (left == 2) batch(line, integral_constant<int, 2>());
+    for (; left >= AHEAD; left -= AHEAD, line += AHEAD * kFewWaves) batch(line, integral_constant<int, AHEAD>());
+    if (AHEAD > 2 && left == 2) batch(line, integral_constant<int, 2>());
     if (left == 1) batch(line, integral_constant<int, 1>());
 #pragma unroll
-    for (int e = 0; e < 16; ++e) lds[wave * kAccLen + e * kAccRow + lane] = acc[e];
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) lds[(wave * F * F + i * F + j) * kAccLen + e * kAccRow + lane] = acc[i][j][e];
     __syncthreads();
-    finish_block<EPI, kFewWaves>(a, lds, kAccLen, tile.mat, tile.m, tile.n, mirror, static_cast<int>(threadIdx.x), kFewWaves * kWave, [] { __syncthreads(); });
+    constexpr int kThreads = kFewWaves * kWave / (F * F);  // to a block
+    const int b = static_cast<int>(threadIdx.x) / kThreads;
+    finish_block<EPI, kFewWaves>(a, lds + b * kAccLen, F * F * kAccLen, tile.mat, tile.m * F + b / F, tile.n * F + b % F, mirror,
+                                 static_cast<int>(threadIdx.x) % kThreads, kThreads, [] { __syncthreads(); });
+}
+
+// ---------------------------------------------------------------- small matrices
+
+// What the three products of a step multiply their sums and their own values by
+struct StepScales {
+    float gram, poly, poly_own, x, x_own;
+};
+
+struct SmallArgs {
+    UpdateArgs u;
+    float unit;                       // of the first X
+    int32_t steps;
+    StepScales by[MQG_ORTH_MAX_STEPS];
+    void *out;
+    int64_t out_row, out_mat;
+    int32_t out_type, step;
+    float keep;
+};
+
+// Word k of lane q of every four lanes becomes word q of lane k.
+__device__ __forceinline__ void quad_transpose(uint32_t (&w)[4]) {
+    const bool odd = lane_id() & 1, upper = lane_id() & 2;
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {                       // with the neighbour: words 0 and 1, 2 and 3
+        const uint32_t out = odd ? w[k] : w[k + 1], in = dpp_u32<0xB1>(out);
+        if (odd) w[k] = in;
+        else w[k + 1] = in;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {                          // with the lane two further: words 0 and 2, 1 and 3
+        const uint32_t out = upper ? w[k] : w[k + 2], in = dpp_u32<0x4E>(out);
+        if (upper) w[k] = in;
+        else w[k + 2] = in;
+    }
+}
+
+// A matrix whose X, X^T and G (then B) fit a compute unit's LDS, all of it in one launch: a workgroup holds it from the update to the
+// weights.  What bounds it is latency: three products of a few blocks per step, with the LDS written between two barriers.
+constexpr int kSmallWaves = 8, kSmallBlocks = 39, kSmallMost = 16;      // blocks of LDS; of X
+inline bool orth_fits_small(int64_t n, int64_t k) {
+    const int64_t nb = ceil_div(n, kSide), kb = ceil_div(k, kSide);
+    return nb * kb <= kSmallMost && 2 * nb * kb + nb * nb <= kSmallBlocks;
+}
+template <typename T>
+__global__ void __launch_bounds__(kSmallWaves * kWave)
+k_orth_small(SmallArgs a) {
+    constexpr int kThreads = kSmallWaves * kWave, kGramEach = 2, kIterateEach = kSmallMost / kSmallWaves;
+    __shared__ __attribute__((aligned(16))) F16 lds[kSmallBlocks * kBlockLen];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), tid = static_cast<int>(threadIdx.x);
+    const int mat = static_cast<int>(blockIdx.x);
+    const int rows = a.u.rows, cols = a.u.cols;
+    const bool tall = rows > cols;
+    const int nb = ((tall ? cols : rows) + kSide - 1) / kSide, kb = ((tall ? rows : cols) + kSide - 1) / kSide;
+    F16 *x = lds, *xt = lds + nb * kb * kBlockLen, *gram = xt + nb * kb * kBlockLen;
+    // the update, row by row of X with a few values between the rows, where X^T will be (and the first KB of G)
+    float *raw = reinterpret_cast<float *>(xt);
+    double *norms = reinterpret_cast<double *>(gram + nb * nb * kBlockLen) - kSmallWaves;
+    const int raw_row = kb * kSide + 4;
+    if (rows * cols < nb * kb * kSide * kSide) {
+        for (int i = tid; i < nb * kSide * raw_row; i += kThreads) raw[i] = 0.f;
+        __syncthreads();
+    }
+    const T *grad = static_cast<const T *>(a.u.grad) + mat * a.u.grad_mat;
+    float *mom = a.u.momentum ? a.u.momentum + mat * a.u.mom_mat : nullptr;
+    double squares = 0.0;
+    constexpr int V = 4, kAhead = 4;                       // vectors of a row on their way together
+    const int vecs = (cols + V - 1) / V, all = rows * vecs;
+    auto four = [&](const auto *row, int i, float (&v)[V]) __attribute__((always_inline)) {
+        using E = std::remove_cv_t<std::remove_pointer_t<decltype(row)>>;
+        typedef E Four __attribute__((ext_vector_type(4)));
+        typedef Four AnyFour __attribute__((aligned(sizeof(E))));
+        if ((i + 1) * V <= cols) {
+            const Four x4 = *reinterpret_cast<const AnyFour *>(row + i * V);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = static_cast<float>(x4[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = i * V + j < cols ? static_cast<float>(row[i * V + j]) : 0.f;
+        }
+    };
+    for (int i0 = tid; i0 < all; i0 += kAhead * kThreads) {
+        float g[kAhead][V], m[kAhead][V];
+        int r[kAhead], i[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int at = i0 + k * kThreads < all ? i0 + k * kThreads : i0;
+            r[k] = static_cast<int>(static_cast<uint32_t>(at) / static_cast<uint32_t>(vecs));
+            i[k] = at - r[k] * vecs;
+            four(grad + r[k] * a.u.grad_row, i[k], g[k]);
+            if (mom) four(mom + r[k] * a.u.mom_row, i[k], m[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (i0 + k * kThreads >= all) break;
+            if (mom) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    m[k][j] = a.u.beta * m[k][j] + g[k][j];
+                    g[k][j] = update_of(a.u, g[k][j], m[k][j]);
+                }
+                store_vec(mom + r[k] * a.u.mom_row, i[k], cols, m[k]);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int c = i[k] * V + j;
+                if (c >= cols) continue;
+                squares += static_cast<double>(g[k][j]) * static_cast<double>(g[k][j]);
+                raw[tall ? c * raw_row + r[k] : r[k] * raw_row + c] = g[k][j];
+            }
+        }
+    }
+    for (int off = 32; off > 0; off >>= 1) squares += __shfl_xor(squares, off, kWave);
+    if (lane == 0) norms[wave] = squares;
+    __syncthreads();
+    squares = 0.0;
+#pragma unroll
+    for (int k = 0; k < kSmallWaves; ++k) squares += norms[k];
+    // unit / (|U| + eps) as a number of 32 bits and a power of two: no product leaves the range of 32 bits on its way
+    int exp = 0;
+    const float inv = static_cast<float>(frexp(static_cast<double>(a.unit) / (sqrt(squares) + static_cast<double>(a.u.eps)), &exp));
+    const int chunks = nb * kb * 128;
+    constexpr int kChunksEach = kSmallMost * 128 / kThreads;
+    auto store_chunk = [&](F16 *to, Half8 hi, Half8 lo) __attribute__((always_inline)) {
+        *reinterpret_cast<Half8 *>(to) = hi;
+        *reinterpret_cast<Half8 *>(to + kTermLen) = lo;
+    };
+    auto chunk_of = [&](const float *from, int step, Half8 *hi, Half8 *lo) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            F16 h, l;
+            split(ldexpf(from[j * step] * inv, exp), &h, &l);
+            (*hi)[j] = h;
+            (*lo)[j] = l;
+        }
+    };
+    Half8 hi[kChunksEach], lo[kChunksEach];
+#pragma unroll
+    for (int e = 0; e < kChunksEach; ++e) {
+        const int u = tid + e * kThreads, b = u / 128, r = u % kSide, c = u / kSide % 4;
+        if (u >= chunks) break;
+        Half8 h, l;
+        chunk_of(raw + (b / kb * kSide + r) * raw_row + b % kb * kSide + 8 * c, 1, &h, &l);            // of X: eight values of a row
+        store_chunk(x + b * kBlockLen + chunk_at(r, c), h, l);
+        chunk_of(raw + (b % nb * kSide + 8 * c) * raw_row + b / nb * kSide + r, raw_row, &hi[e], &lo[e]);      // of X^T: eight rows of a column
+    }
+    __syncthreads();                                       // X^T in the place of the update
+#pragma unroll
+    for (int e = 0; e < kChunksEach; ++e) {
+        const int u = tid + e * kThreads;
+        if (u >= chunks) break;
+        store_chunk(xt + u / 128 * kBlockLen + chunk_at(u % kSide, u / kSide % 4), hi[e], lo[e]);
+    }
+    __syncthreads();
+
+    int own_lane = lane;              // made new in every step: the compiler would keep the addresses of all of a step's accesses, 256 registers and more
+    // sum over `deep` neighbouring blocks of P and Q
+    auto product = [&](const F16 *p, const F16 *q, int deep) __attribute__((always_inline)) {
+        Float16v acc{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+        for (int d = 0; d < deep; ++d) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const F16 *pb = p + d * kBlockLen + t * 512 + own_lane * 8, *qb = q + d * kBlockLen + t * 512 + own_lane * 8;
+                const Half8 ph = *reinterpret_cast<const Half8 *>(pb), pl = *reinterpret_cast<const Half8 *>(pb + kTermLen);
+                const Half8 qh = *reinterpret_cast<const Half8 *>(qb), ql = *reinterpret_cast<const Half8 *>(qb + kTermLen);
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
+            }
+        }
+        return acc;
+    };
+    // Registers 4 c ... 4 c + 3 of a lane are four neighbouring values, half of chunk c, of row lane % 32 of the block turned
+    auto turned_at = [&](F16 *block, int c) __attribute__((always_inline)) { return block + chunk_at(own_lane & 31, c) + 4 * (own_lane >> 5); };
+    auto store_turned = [&](F16 *block, const Float16v &v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            Half4 hi, lo;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                F16 h, l;
+                split(v[4 * c + j], &h, &l);
+                hi[j] = h;
+                lo[j] = l;
+            }
+            *reinterpret_cast<Half4 *>(turned_at(block, c)) = hi;
+            *reinterpret_cast<Half4 *>(turned_at(block, c) + kTermLen) = lo;
+        }
+    };
+    auto add_own = [&](Float16v &v, float by, F16 *block, float own_by) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const Half4 hi = *reinterpret_cast<const Half4 *>(turned_at(block, c)), lo = *reinterpret_cast<const Half4 *>(turned_at(block, c) + kTermLen);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * c + j] = by * v[4 * c + j] + own_by * (static_cast<float>(hi[j]) + static_cast<float>(lo[j]));
+        }
+    };
+    Float16v v[kIterateEach];
+#pragma unroll 1
+    for (int s = 0;; ++s) {
+        const StepScales by = a.by[s];
+        asm volatile("" : "+v"(own_lane));
+        for (int b = wave; b < nb * nb; b += kSmallWaves) {                  // G: every block is computed, and stored turned
+            const int i = b / nb, j = b % nb;
+            Float16v g = product(x + i * kb * kBlockLen, x + j * kb * kBlockLen, kb);
+            g *= by.gram;
+            store_turned(gram + (j * nb + i) * kBlockLen, g);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kGramEach; ++e) {
+            const int b = wave + e * kSmallWaves, i = b / nb, j = b % nb;
+            if (b >= nb * nb) continue;
+            v[e] = product(gram + i * nb * kBlockLen, gram + j * nb * kBlockLen, nb);
+            add_own(v[e], by.poly, gram + (j * nb + i) * kBlockLen, by.poly_own);
+        }
+        __syncthreads();                                   // B in the place of G
+#pragma unroll
+        for (int e = 0; e < kGramEach; ++e) {
+            const int b = wave + e * kSmallWaves;
+            if (b < nb * nb) store_turned(gram + (b % nb * nb + b / nb) * kBlockLen, v[e]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kIterateEach; ++e) {           // block (i, j) of X
+            const int b = wave + e * kSmallWaves, i = b / kb, j = b % kb;
+            if (b >= nb * kb) continue;
+            v[e] = product(gram + i * nb * kBlockLen, xt + j * nb * kBlockLen, nb);
+            add_own(v[e], by.x, xt + (j * nb + i) * kBlockLen, by.x_own);
+        }
+        if (s + 1 == a.steps) break;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kIterateEach; ++e) {
+            const int b = wave + e * kSmallWaves, i = b / kb, j = b % kb;
+            if (b >= nb * kb) continue;
+            store_turned(xt + (j * nb + i) * kBlockLen, v[e]);
+            // as it lies: four lanes exchange their four rows of a column each for a row of four columns each
+            F16 *block = x + b * kBlockLen + chunk_at(4 * (own_lane >> 5) + (own_lane & 3), (own_lane & 31) / 8) + (own_lane & 4);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    F16 h, l;
+                    split(v[e][4 * c + k], &h, &l);
+                    w[k] = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, h)) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, l)) << 16;
+                }
+                quad_transpose(w);
+                typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
+                F16 *to = block + 8 * 8 * c;
+                *reinterpret_cast<Words2 *>(to) = Words2{(w[0] & 0xFFFFu) | w[1] << 16, (w[2] & 0xFFFFu) | w[3] << 16};
+                *reinterpret_cast<Words2 *>(to + kTermLen) = Words2{w[0] >> 16 | (w[1] & 0xFFFF0000u), w[2] >> 16 | (w[3] & 0xFFFF0000u)};
+            }
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int e = 0; e < kIterateEach; ++e) {
+        const int b = wave + e * kSmallWaves, i = b / kb, j = b % kb;
+        if (b >= nb * kb) continue;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int m = i * kSide + 8 * (k / 4) + 4 * (lane >> 5) + k % 4, n = j * kSide + (lane & 31);
+            const int r = tall ? n : m, c = tall ? m : n;
+            if (r >= rows || c >= cols) continue;
+            const int64_t at = mat * a.out_mat + r * a.out_row + c;
+            if (a.step) {
+                float *w = static_cast<float *>(a.out) + at;
+                *w = a.keep * *w + v[e][k];
+            } else if (a.out_type == MQG_F16) {
+                static_cast<F16 *>(a.out)[at] = static_cast<F16>(v[e][k]);
+            } else if (a.out_type == MQG_BF16) {
+                static_cast<BF16 *>(a.out)[at] = static_cast<BF16>(v[e][k]);
+            } else {
+                static_cast<float *>(a.out)[at] = v[e][k];
+            }
+        }
+    }
 }
 
 // ---------------------------------------------------------------- host side
@@ -477,19 +776,31 @@ int unit_exp(double most) {
     return 15 - e;
 }
 
-constexpr int kFewSide = 512;          // smaller sides up to this: see launch_product
-constexpr int kOrthTile = 128, kOrthPad = kSplitTile;
+// Which kernel makes a product, by the tiles of 64 x 64 that it has, both halves of a symmetric one counted.  Times in us by events of single blocks
+// (kBlocks), tiles of 64 and of 128:  1,024^2 G 13.7, 13.4, 28, X 17.4, 14.6, 31;  512^2 7.3, 9.6, 19 and 8.3, 10.2, 20;  512 x 4,096 16, 32, 85 and 21, 18, 24;
+// two of 1,024^2 18.5, 21.7, 29 and 28, 23, 33;  four 29.5, 30.5, 31.5 and 51, 42, 38;  eight 53, 48, 51 and 99, 80, 63;  1,536^2 25, 28, 39 and 43, 42, 44;  2,048^2 52, 52, 50
+// and 91, 71, 62;  4,096^2 366, 268, 218 and 728, 529, 397.  (Tiles of 64 through LDS with two to five blocks ahead: as those of 64 in all of these.)
+enum Kernel { kBlocks, kTiles64, kTiles128 };
+Kernel kernel_for(bool symmetric, int64_t m, int64_t n, int64_t mats) {
+    const int64_t tiles = ceil_div(m, 64) * ceil_div(n, 64) * mats;
+    if (tiles <= (symmetric ? 600 : 144)) return kBlocks;
+    return tiles <= (symmetric ? 2048 : 768) ? kTiles64 : kTiles128;
+}
+
 constexpr int kOrthParts = 1024;      // workgroups per matrix that share its norm
 
 struct OrthLayout {
     int64_t n, k;                     // padded
     int64_t x, g;                     // f16 of a matrix
     int64_t parts, bytes;
+    Kernel gram_kernel, x_kernel;
 };
 OrthLayout orth_layout(int64_t mats, int64_t rows, int64_t cols) {
     OrthLayout l;
     const int64_t n = std::min(rows, cols), k = std::max(rows, cols);
-    const int64_t pad = n > kFewSide ? kOrthTile : kOrthPad;
+    l.gram_kernel = kernel_for(true, n, n, mats);
+    l.x_kernel = kernel_for(false, n, k, mats);
+    const int64_t pad = l.gram_kernel == kTiles128 || l.x_kernel == kTiles128 ? 128 : 64;
     l.n = ceil_div(n, pad) * pad;
     l.k = ceil_div(k, pad) * pad;
     l.x = l.n * l.k * 2;
@@ -499,30 +810,35 @@ OrthLayout orth_layout(int64_t mats, int64_t rows, int64_t cols) {
     return l;
 }
 
-// Two tiles of 128 x 128 fit a compute unit.  A few tiles more than whole rounds of the chip would take as long as a round; up to kTileRest of
-// them go block by block, their depth shared by the wavefronts.
+// Two tiles of 128 x 128 fit a compute unit.  A few tiles more than whole rounds of the chip would take as long as a round (4,096 rows: 528
+// tiles, G of 8,192 values 534 us); up to kTileRest of them go block by block, their depth shared by the wavefronts (387 and 30).
 constexpr int kTileRound = 512, kTileRest = 64;
 template <int EPI>
-int launch_product(mqg_ctx *ctx, ProductArgs a, int64_t mats, bool few, hipStream_t s) {
+int launch_product(mqg_ctx *ctx, ProductArgs a, int64_t mats, Kernel kernel, hipStream_t s) {
     static const char *const names[] = {"k_orth_gram", "k_orth_poly", "k_orth_iterate", "k_orth_out"};
     constexpr bool symmetric = EPI == kGram || EPI == kPoly;
     auto tiles_of = [&](int side) {
         a.tiles_m = a.m / side;
         a.tiles_n = a.n / side;
         a.tiles = symmetric ? static_cast<int32_t>(int64_t(a.tiles_m) * (a.tiles_m + 1) / 2) : a.tiles_m * a.tiles_n;
-        return int64_t(a.tiles) * mats;
+        return static_cast<int>(a.tiles * mats);
     };
-    if (few) {
-        const int grid = static_cast<int>(tiles_of(kSide));
-        MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product_few<EPI, 1><<<grid, kFewWaves * kWave, 0, s>>>(a)));
+    if (kernel == kBlocks) {
+        const int grid = tiles_of(kSide);
+        MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product_few<EPI, 1, 1, 3><<<grid, kFewWaves * kWave, 0, s>>>(a)));
         return MQG_OK;
     }
-    const int all = static_cast<int>(tiles_of(kOrthTile)), rest = all > kTileRound && all % kTileRound <= kTileRest ? all % kTileRound : 0;
+    if (kernel == kTiles64) {
+        const int grid = tiles_of(64);
+        MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product_few<EPI, 1, 2, 2><<<grid, kFewWaves * kWave, 0, s>>>(a)));
+        return MQG_OK;
+    }
+    const int all = tiles_of(128), rest = all > kTileRound && all % kTileRound <= kTileRest ? all % kTileRound : 0;
     MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product<EPI, 2, 2, 2, 2><<<all - rest, 256, 0, s>>>(a)));
     if (rest) {
-        constexpr int sub = kOrthTile / kSide;
+        constexpr int sub = 128 / kSide;
         a.first_tile = all - rest;
-        MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product_few<EPI, sub><<<rest * sub * sub, kFewWaves * kWave, 0, s>>>(a)));
+        MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product_few<EPI, sub, 1, 3><<<rest * sub * sub, kFewWaves * kWave, 0, s>>>(a)));
     }
     return MQG_OK;
 }
@@ -546,24 +862,57 @@ bool orth_coeffs_fit(const float *coeffs, int32_t steps) {
 
 int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
     const int64_t mats = call.mats, rows = call.rows, cols = call.cols;
-    const OrthLayout l = orth_layout(mats, rows, cols);
-    int rc = ensure_layer_scratch(ctx, l.bytes, s, call.who);
-    if (rc != MQG_OK) return rc;
-    double *parts = reinterpret_cast<double *>(ctx->layer_scratch);
-    F16 *x = reinterpret_cast<F16 *>(ctx->layer_scratch + l.parts);          // X: n rows of k values
-    F16 *xt[2] = {x + mats * l.x, x + 2 * mats * l.x};                       // its transpose, in turns
-    F16 *gram = x + 3 * mats * l.x, *poly = gram + mats * l.g;
-    const bool tall = rows > cols, few = std::min(rows, cols) <= kFewSide;
-
-    UpdateArgs u{call.grad, call.momentum, call.grad_row, call.grad_mat, call.mom_row, call.mom_mat, parts, static_cast<int32_t>(rows),
+    UpdateArgs u{call.grad, call.momentum, call.grad_row, call.grad_mat, call.mom_row, call.mom_mat, nullptr, static_cast<int32_t>(rows),
                  static_cast<int32_t>(cols), call.nesterov, call.beta, call.eps};
+    // the powers of two that X, G and B are stored times, step by step
+    StepScales by[MQG_ORTH_MAX_STEPS];
     double r = 1.0;
     int ex = unit_exp(r);
     const float unit = std::ldexp(1.f, ex);
+    for (int i = 0; i < call.steps; ++i) {
+        const float *k = call.coeffs + 3 * i;
+        const bool last = i + 1 == call.steps;
+        const int eg = unit_exp(r * r), eb = unit_exp(gram_poly_most(k, r));
+        r = poly_most(k, r) * 1.001;
+        const int next = last ? 0 : unit_exp(r);
+        const float out_by = last ? call.out_by : 1.f;
+        by[i] = {std::ldexp(1.f, eg - 2 * ex), k[2] * std::ldexp(1.f, eb - 2 * eg), k[1] * std::ldexp(1.f, eb - eg),
+                 out_by * std::ldexp(1.f, next - eb - ex), out_by * k[0] * std::ldexp(1.f, next - ex)};
+        ex = next;
+    }
+    auto typed = [&](auto go) { return call.dtype == MQG_F16 ? go(F16()) : call.dtype == MQG_BF16 ? go(BF16()) : go(float()); };
+
+    if (orth_fits_small(std::min(rows, cols), std::max(rows, cols))) {
+        SmallArgs a{};
+        a.u = u;
+        a.unit = unit;
+        a.steps = call.steps;
+        std::copy(by, by + call.steps, a.by);
+        a.out = call.out;
+        a.out_row = call.out_row;
+        a.out_mat = call.out_mat;
+        a.out_type = call.out_type;
+        a.step = call.step;
+        a.keep = call.keep;
+        return typed([&](auto type) -> int {
+            using T = decltype(type);
+            MQG_LAUNCH(ctx, "k_orth_small", s, (k_orth_small<T><<<static_cast<int>(mats), kSmallWaves * kWave, 0, s>>>(a)));
+            return MQG_OK;
+        });
+    }
+
+    const OrthLayout l = orth_layout(mats, rows, cols);
+    int rc = ensure_layer_scratch(ctx, l.bytes, s, call.who);
+    if (rc != MQG_OK) return rc;
+    u.parts = reinterpret_cast<double *>(ctx->layer_scratch);
+    F16 *x = reinterpret_cast<F16 *>(ctx->layer_scratch + l.parts);          // X: n rows of k values
+    F16 *xt[2] = {x + mats * l.x, x + 2 * mats * l.x};                       // its transpose, in turns
+    F16 *gram = x + 3 * mats * l.x, *poly = gram + mats * l.g;
+    const bool tall = rows > cols;
     const int64_t pad_rows = tall ? l.k : l.n, pad_cols = tall ? l.n : l.k;
     const dim3 split_grid(static_cast<uint32_t>(pad_cols / kSplitTile), static_cast<uint32_t>(pad_rows / kSplitTile), static_cast<uint32_t>(mats));
     F16 *same = tall ? xt[0] : x, *turned = tall ? x : xt[0];
-    auto begin = [&](auto type) -> int {
+    rc = typed([&](auto type) -> int {
         using T = decltype(type);
         const int64_t vecs = rows * ceil_div(cols, Vec<T>::kLen);
         const int nparts = static_cast<int>(std::min<int64_t>(ceil_div(vecs, kBlock), kOrthParts));
@@ -572,13 +921,10 @@ int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
         MQG_LAUNCH(ctx, "k_orth_split", s,
                    (k_orth_split<T><<<split_grid, kBlock, 0, s>>>(u, nparts, unit, same, turned, static_cast<int>(pad_rows), static_cast<int>(pad_cols))));
         return MQG_OK;
-    };
-    rc = call.dtype == MQG_F16 ? begin(F16()) : call.dtype == MQG_BF16 ? begin(BF16()) : begin(float());
+    });
     if (rc != MQG_OK) return rc;
 
     for (int i = 0; i < call.steps; ++i) {
-        const float *k = call.coeffs + 3 * i;
-        const int eg = unit_exp(r * r), eb = unit_exp(gram_poly_most(k, r));
         ProductArgs a{};
         a.p = a.q = x;
         a.p_mat = a.q_mat = l.x;
@@ -586,26 +932,22 @@ int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
         a.m = a.n = static_cast<int32_t>(l.n);
         a.to = a.to_turned = gram;
         a.to_mat = l.g;
-        a.acc_by = std::ldexp(1.f, eg - 2 * ex);
-        rc = launch_product<kGram>(ctx, a, mats, few, s);
+        a.acc_by = by[i].gram;
+        rc = launch_product<kGram>(ctx, a, mats, l.gram_kernel, s);
         if (rc != MQG_OK) return rc;
 
         a.p = a.q = a.own = gram;
         a.p_mat = a.q_mat = a.own_mat = l.g;
         a.depth = static_cast<int32_t>(l.n);
         a.to = a.to_turned = poly;
-        a.acc_by = k[2] * std::ldexp(1.f, eb - 2 * eg);
-        a.own_by = k[1] * std::ldexp(1.f, eb - eg);
-        rc = launch_product<kPoly>(ctx, a, mats, few, s);
+        a.acc_by = by[i].poly;
+        a.own_by = by[i].poly_own;
+        rc = launch_product<kPoly>(ctx, a, mats, l.gram_kernel, s);
         if (rc != MQG_OK) return rc;
 
-        r = poly_most(k, r) * 1.001;
-        const bool last = i + 1 == call.steps;
-        const int next = last ? 0 : unit_exp(r);
         F16 *const now = xt[i & 1], *const then = xt[~i & 1];
-        const float by = last ? call.out_by : 1.f;
-        a.acc_by = by * std::ldexp(1.f, next - eb - ex);
-        a.own_by = by * k[0] * std::ldexp(1.f, next - ex);
+        a.acc_by = by[i].x;
+        a.own_by = by[i].x_own;
         // B X as it lies, or, for a tall U, its transpose X^T B: rows of the product are rows of U, so that the output is written along its rows
         a.p = tall ? now : poly;
         a.p_mat = tall ? l.x : l.g;
@@ -617,8 +959,8 @@ int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
         a.to_turned = tall ? x : then;
         a.m = static_cast<int32_t>(tall ? l.k : l.n);
         a.n = static_cast<int32_t>(tall ? l.n : l.k);
-        if (!last) {
-            rc = launch_product<kIterate>(ctx, a, mats, few, s);
+        if (i + 1 < call.steps) {
+            rc = launch_product<kIterate>(ctx, a, mats, l.x_kernel, s);
         } else {
             a.out = call.out;
             a.out_row = call.out_row;
@@ -628,10 +970,9 @@ int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
             a.out_type = call.out_type;
             a.step = call.step;
             a.keep = call.keep;
-            rc = launch_product<kOut>(ctx, a, mats, few, s);
+            rc = launch_product<kOut>(ctx, a, mats, l.x_kernel, s);
         }
         if (rc != MQG_OK) return rc;
-        ex = next;
     }
     return MQG_OK;
 }
