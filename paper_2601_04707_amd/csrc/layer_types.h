@@ -19,6 +19,20 @@ struct Vec {
     typedef Whole Any __attribute__((aligned(sizeof(T))));
 };
 
+// Vector number i of a row of dim elements, zeros past its end; nothing outside the row is read.
+template <typename T>
+__device__ __forceinline__ typename Vec<T>::Whole load_raw(const T *row, int i, int dim) {
+    constexpr int V = Vec<T>::kLen;
+    typename Vec<T>::Whole v;
+    if ((i + 1) * V <= dim) {
+        v = *reinterpret_cast<const typename Vec<T>::Any *>(row + i * V);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = i * V + j < dim ? row[i * V + j] : static_cast<T>(0.f);
+    }
+    return v;
+}
+
 // Vector number i of a row of dim elements as 32-bit numbers, zeros past its end; nothing outside the row is read.
 template <typename T>
 __device__ __forceinline__ void load_vec(const T *row, int i, int dim, float (&out)[Vec<T>::kLen]) {
@@ -33,19 +47,33 @@ __device__ __forceinline__ void load_vec(const T *row, int i, int dim, float (&o
     }
 }
 
-// The same vector of a row that is written: rounded once, to nearest even; nothing outside the row is written.
-template <typename T>
+// The same vector of a row that is written: rounded once, to nearest even; nothing outside the row is written.  PAST: not to be kept in the caches
+// (a template's argument: of a branch on it the compiler makes one store of the usual kind)
+template <bool PAST = false, typename T>
 __device__ __forceinline__ void store_vec(T *row, int i, int dim, const float (&in)[Vec<T>::kLen]) {
     constexpr int V = Vec<T>::kLen;
     if ((i + 1) * V <= dim) {
         typename Vec<T>::Whole v;
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = static_cast<T>(in[j]);
-        *reinterpret_cast<typename Vec<T>::Any *>(row + i * V) = v;
+        if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<typename Vec<T>::Any *>(row + i * V));
+        else *reinterpret_cast<typename Vec<T>::Any *>(row + i * V) = v;
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)
             if (i * V + j < dim) row[i * V + j] = static_cast<T>(in[j]);
+    }
+}
+
+// Columns i V to i V + V - 1 of a [dim] vector of floats, zeros past its end; null: ones
+template <int V>
+__device__ __forceinline__ void load_weight(const float *w, int i, int dim, float (&out)[V]) {
+#pragma unroll
+    for (int h = 0; h < V / 4; ++h) {
+        float x[4] = {1.f, 1.f, 1.f, 1.f};
+        if (w) load_vec(w, i * (V / 4) + h, dim, x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[4 * h + j] = x[j];
     }
 }
 

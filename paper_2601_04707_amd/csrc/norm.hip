@@ -15,7 +15,7 @@
 
 namespace mqg {
 
-constexpr int kNormParts = 1024;      // workgroups of a backward at most
+constexpr int kNormParts = 512;      // workgroups of a backward at most
 
 int64_t norm_scratch_bytes(int32_t dim) { return int64_t(kNormParts) * dim * int64_t(sizeof(float)); }
 
@@ -58,6 +58,28 @@ struct RowLanes {
 #pragma unroll
         for (int k = 1; k < kWaves; ++k) all = f(all, buf[k]);
         return all;
+    }
+    // two sums by one exchange (of buffers of twice the size; not with the others in one kernel)
+    __device__ __forceinline__ void sum_both(float *x, float *y) {
+        *x = lanes_sum(*x, LANES < kWave ? LANES : kWave);
+        *y = lanes_sum(*y, LANES < kWave ? LANES : kWave);
+        if constexpr (LANES > kWave) {
+            float *buf = lds + turn * 2 * kWaves;
+            turn ^= 1;
+            if (lane_id() == 0) {
+                buf[2 * (threadIdx.x >> 6)] = *x;
+                buf[2 * (threadIdx.x >> 6) + 1] = *y;
+            }
+            __syncthreads();
+            float u = 0.f, v = 0.f;
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) {
+                u += buf[2 * k];
+                v += buf[2 * k + 1];
+            }
+            *x = u;
+            *y = v;
+        }
     }
     __device__ __forceinline__ float sum(float v) {
         v = lanes_sum(v, LANES < kWave ? LANES : kWave);
@@ -120,7 +142,7 @@ __device__ __forceinline__ void store_q(uint8_t *row, int i, int dim, const floa
     }
 }
 
-template <typename T, int LANES, int NV>
+template <typename T, int LANES, int NV, bool PAST>
 __global__ void __launch_bounds__(LANES > kBlock ? LANES : kBlock)
 k_rms_norm(NormArgs a) {
     constexpr int V = Vec<T>::kLen;
@@ -135,12 +157,7 @@ k_rms_norm(NormArgs a) {
     const int group_lanes = a.group / V;                   // lanes that share a scale, 0 = the row's
     float w[NV][V];
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c = (k * LANES + lane) * V + j;
-            w[k][j] = !a.weight ? 1.f : c < dim ? a.weight[c] : 0.f;
-        }
+    for (int k = 0; k < NV; ++k) load_weight(a.weight, k * LANES + lane, dim, w[k]);
     for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; row < n; row += int64_t(gridDim.x) * kRows) {
         float s[NV][V];
         const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
@@ -159,7 +176,7 @@ k_rms_norm(NormArgs a) {
         if (a.sum) {
             T *sum = static_cast<T *>(a.sum) + row * a.sum_stride;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) store_vec(sum, k * LANES + lane, dim, s[k]);
+            for (int k = 0; k < NV; ++k) store_vec<PAST>(sum, k * LANES + lane, dim, s[k]);
         }
         float squares = 0.f;
 #pragma unroll
@@ -178,7 +195,7 @@ k_rms_norm(NormArgs a) {
         if (a.y) {
             T *y = static_cast<T *>(a.y) + row * a.y_stride;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) store_vec(y, k * LANES + lane, dim, s[k]);
+            for (int k = 0; k < NV; ++k) store_vec<PAST>(y, k * LANES + lane, dim, s[k]);
         }
         if (!a.q) continue;
         uint8_t *q = a.q + row * a.q_stride;
@@ -223,75 +240,81 @@ struct NormGradArgs {
     int32_t dim;
 };
 
-template <typename T, int LANES, int NV>
+template <typename T, int LANES, int NV, bool PAST>
 __global__ void __launch_bounds__(LANES > kBlock ? LANES : kBlock)
 k_rms_norm_backward(NormGradArgs a) {
+    using W = typename Vec<T>::Whole;
     constexpr int V = Vec<T>::kLen;
     constexpr int kThreads = LANES > kBlock ? LANES : kBlock;
     constexpr int kRows = kThreads / LANES;
     constexpr int kCols = LANES * NV * V;
     // rows of several wavefronts: their exchange; others: the wavefronts' sums of the weight's gradient
-    __shared__ float lds[LANES > kWave ? 2 * (LANES / kWave) : kWavesPerBlock * kCols];
+    __shared__ float lds[LANES > kWave ? 4 * (LANES / kWave) : kWavesPerBlock * kCols];
     RowLanes<LANES> lanes(lds);
     const int lane = static_cast<int>(threadIdx.x) % LANES;
     const int64_t n = rows_of(a.num_rows, a.cap_rows);
     const int dim = a.dim;
     float w[NV][V], gw[NV][V];
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+        load_weight(a.weight, k * LANES + lane, dim, w[k]);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c = (k * LANES + lane) * V + j;
-            w[k][j] = !a.weight ? 1.f : c < dim ? a.weight[c] : 0.f;
-            gw[k][j] = 0.f;
-        }
-    for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; row < n; row += int64_t(gridDim.x) * kRows) {
-        float s[NV][V], g[NV][V];
+        for (int j = 0; j < V; ++j) gw[k][j] = 0.f;
+    }
+    struct Row {
+        W s[NV], g[NV], gs[NV];
+    };
+    auto load = [&](int64_t row) __attribute__((always_inline)) {
+        Row v;
         const T *sr = static_cast<const T *>(a.s) + row * a.s_stride;
         const T *gr = static_cast<const T *>(a.grad_y) + row * a.gy_stride;
+        const T *gs = static_cast<const T *>(a.grad_sum) + row * a.gs_stride;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            load_vec(sr, k * LANES + lane, dim, s[k]);
-            load_vec(gr, k * LANES + lane, dim, g[k]);
+            v.s[k] = load_raw(sr, k * LANES + lane, dim);
+            v.g[k] = load_raw(gr, k * LANES + lane, dim);
+            if (a.grad_sum) v.gs[k] = load_raw(gs, k * LANES + lane, dim);
         }
+        return v;
+    };
+    // A row is on its way while the one before is worked on, if the registers hold both.
+    constexpr bool kAhead = kThreads < 1024 || NV * V < 16;
+    const int64_t step = int64_t(gridDim.x) * kRows;
+    int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES;
+    Row next;
+    if (kAhead && row < n) next = load(row);
+    for (; row < n; row += step) {
+        const Row v = kAhead ? next : load(row);
+        if (kAhead && row + step < n) next = load(row + step);
         float squares = 0.f, dot = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             float p = 0.f, d = 0.f;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                p += s[k][j] * s[k][j];
-                d += g[k][j] * w[k][j] * s[k][j];
+                const float s = static_cast<float>(v.s[k][j]);
+                p += s * s;
+                d += static_cast<float>(v.g[k][j]) * w[k][j] * s;
             }
             squares += p;
             dot += d;
         }
-        squares = lanes.sum(squares);
-        dot = lanes.sum(dot);
+        lanes.sum_both(&squares, &dot);
         const float r = 1.0f / sqrtf(squares / static_cast<float>(dim) + a.eps);
         const float c = r * r * (dot / static_cast<float>(dim));
-        if (a.parts) {
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j) gw[k][j] += g[k][j] * (s[k][j] * r);
-        }
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int j = 0; j < V; ++j) g[k][j] = r * (g[k][j] * w[k][j] - c * s[k][j]);
-        if (a.grad_sum) {
-            const T *gs = static_cast<const T *>(a.grad_sum) + row * a.gs_stride;
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                load_vec(gs, k * LANES + lane, dim, s[k]);
-#pragma unroll
-                for (int j = 0; j < V; ++j) g[k][j] += s[k][j];
-            }
-        }
         T *gx = static_cast<T *>(a.grad_x) + row * a.gx_stride;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) store_vec(gx, k * LANES + lane, dim, g[k]);
+        for (int k = 0; k < NV; ++k) {
+            float out[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float s = static_cast<float>(v.s[k][j]), g = static_cast<float>(v.g[k][j]);
+                gw[k][j] += g * (s * r);
+                out[j] = r * (g * w[k][j] - c * s);
+                if (a.grad_sum) out[j] += static_cast<float>(v.gs[k][j]);
+            }
+            store_vec<PAST>(gx, k * LANES + lane, dim, out);
+        }
     }
     if (!a.parts) return;
     float *part = a.parts + int64_t(blockIdx.x) * dim;
@@ -324,37 +347,50 @@ k_rms_norm_backward(NormGradArgs a) {
     }
 }
 
-// out[c] = sum over the parts, 16 columns a workgroup: 16 threads take a column's parts in turn and their sums are added in order.
-constexpr int kSumCols = 16;
-__global__ void __launch_bounds__(kBlock)
+// out[c] = sum over the parts, 16 columns a workgroup: 64 threads take a column's parts in turn, eight of them on their way together, and their sums are
+// added in order.
+constexpr int kSumCols = 16, kSumThreads = 1024;
+__global__ void __launch_bounds__(kSumThreads)
 k_sum_parts(const float *__restrict__ parts, int num_parts, int dim, float *__restrict__ out) {
-    constexpr int kTurns = kBlock / kSumCols;
-    __shared__ float lds[kTurns][kSumCols];
+    constexpr int kTurns = kSumThreads / kSumCols, kAhead = 8;
+    __shared__ float lds[kTurns][kSumCols + 1];
     const int c = static_cast<int>(blockIdx.x) * kSumCols + static_cast<int>(threadIdx.x) % kSumCols;
     const int turn = static_cast<int>(threadIdx.x) / kSumCols;
     float v = 0.f;
     if (c < dim)
-        for (int p = turn; p < num_parts; p += kTurns) v += parts[int64_t(p) * dim + c];
+        for (int p0 = turn; p0 < num_parts; p0 += kAhead * kTurns) {
+            float x[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) x[k] = p0 + k * kTurns < num_parts ? parts[int64_t(p0 + k * kTurns) * dim + c] : 0.f;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) v += x[k];
+        }
     lds[turn][threadIdx.x % kSumCols] = v;
     __syncthreads();
-    if (turn == 0 && c < dim) {
-        v = lds[0][threadIdx.x];
-#pragma unroll
-        for (int k = 1; k < kTurns; ++k) v += lds[k][threadIdx.x];
-        out[c] = v;
-    }
+    // the 64 sums of a column by the lanes of a wavefront
+    const int col = static_cast<int>(threadIdx.x) / kWave;
+    v = lanes_sum(lds[lane_id()][col], kWave);
+    if (lane_id() == 0 && static_cast<int>(blockIdx.x) * kSumCols + col < dim) out[static_cast<int>(blockIdx.x) * kSumCols + col] = v;
 }
+static_assert(kSumThreads / kSumCols == kWave && kSumThreads / kWave == kSumCols, "a wavefront adds a column");
 
-// How a row is laid out: lanes, and vectors per lane
+// How a row is laid out: lanes, and vectors per lane.  As few lanes as hold it with up to four vectors each within a wavefront; longer rows have a
+// workgroup of 512 (8,192 rows of 8,192 bf16: 109 us and the backward 112; 256 lanes 144 and 112, 1,024 126 and 120), the longest one of 1,024.
+// Few rows are spread as wide as they go: there is nothing else to do.
 struct RowShape {
     int lanes, nv;
 };
-RowShape row_shape(int dim, int vec) {
+constexpr int kFewRows = 256;
+RowShape row_shape(int dim, int vec, int64_t rows) {
     const int vecs = static_cast<int>(ceil_div(dim, vec));
     for (int lanes = 4; lanes <= kWave; lanes <<= 1)
         if (vecs <= lanes) return {lanes, 1};
+    if (rows <= kFewRows) {
+        if (vecs <= 256) return {256, 1};
+        if (vecs > 512 && vecs <= 1024) return {1024, 1};
+    }
     if (vecs <= 4 * kWave) return {kWave, static_cast<int>(ceil_div(vecs, kWave))};
-    if (vecs <= 4 * 256) return {256, vecs <= 2 * 256 ? 2 : 4};
+    if (vecs <= 2 * 512) return {512, static_cast<int>(ceil_div(vecs, 512))};
     return {1024, vecs <= 2 * 1024 ? 2 : 4};
 }
 
@@ -370,21 +406,36 @@ RowShape row_shape(int dim, int vec) {
             else if (sh.nv == 3) GO(T, 64, 3);                     \
             else GO(T, 64, 4);                                     \
             break;                                                 \
-        case 256:                                                  \
-            if (sh.nv == 2) GO(T, 256, 2);                         \
-            else GO(T, 256, 4);                                    \
+        case 256: GO(T, 256, 1); break;                            \
+        case 512:                                                  \
+            if (sh.nv == 1) GO(T, 512, 1);                         \
+            else GO(T, 512, 2);                                    \
             break;                                                 \
         default:                                                   \
-            if (sh.nv == 2) GO(T, 1024, 2);                        \
+            if (sh.nv == 1) GO(T, 1024, 1);                        \
+            else if (sh.nv == 2) GO(T, 1024, 2);                   \
             else if constexpr (sizeof(T) == 4) GO(T, 1024, 4);     \
     }
 
+// A call that moves twice what the chip's memory-side cache holds leaves little of its own output there: that goes past the caches (109,000 x 602
+// fp32 rows, four times 262 MB: 213 -> 201 us; 295,000 x 256 fp16 109 -> 102).  Smaller ones keep it for the next reader.
+constexpr int64_t kPastBytes = int64_t(512) << 20;
+
 template <typename T>
 int launch_norm(mqg_ctx *ctx, const NormArgs &a, hipStream_t s) {
-    const RowShape sh = row_shape(a.dim, Vec<T>::kLen);
+    const RowShape sh = row_shape(a.dim, Vec<T>::kLen, a.cap_rows);
+    const int64_t cells = a.cap_rows * a.dim, arrays = 1 + (a.residual != nullptr) + (a.sum != nullptr) + (a.y != nullptr);
+    const bool past = cells * (arrays * int64_t(sizeof(T)) + (a.q != nullptr)) >= kPastBytes;
     const int threads = std::max(sh.lanes, kBlock);
-    const int grid = static_cast<int>(std::min<int64_t>(ceil_div(a.cap_rows, threads / sh.lanes), int64_t(256) * 8 * kBlock / threads));
-#define MQG_GO(T, L, N) MQG_LAUNCH(ctx, "k_rms_norm", s, (k_rms_norm<T, L, N><<<grid, threads, 0, s>>>(a)))
+    // A workgroup takes one set of rows (loops of a few workgroups per compute unit read at 4.2 to 5.2 TB/s, this at 4.9 to 5.9), of 16-bit rows, whose weight is
+    // twice as long as they are, several (295,000 x 256 fp16: 118 us with one, 109 with 4.5, 131 with 18).
+    const int64_t most = sizeof(T) == 4 ? (int64_t(1) << 31) - 1 : int64_t(8192) * kBlock / threads;
+    const int64_t grid = std::min<int64_t>(std::min<int64_t>(ceil_div(a.cap_rows, threads / sh.lanes), most), ((int64_t(1) << 32) - 1) / threads);
+#define MQG_GO(T, L, N)                                                                                                        \
+    do {                                                                                                                       \
+        if (past) MQG_LAUNCH(ctx, "k_rms_norm", s, (k_rms_norm<T, L, N, true><<<static_cast<uint32_t>(grid), threads, 0, s>>>(a)));  \
+        else MQG_LAUNCH(ctx, "k_rms_norm", s, (k_rms_norm<T, L, N, false><<<static_cast<uint32_t>(grid), threads, 0, s>>>(a)));      \
+    } while (0)
     MQG_NORM_SHAPES(T, MQG_GO)
 #undef MQG_GO
     return MQG_OK;
@@ -392,22 +443,27 @@ int launch_norm(mqg_ctx *ctx, const NormArgs &a, hipStream_t s) {
 
 template <typename T>
 int launch_norm_backward(mqg_ctx *ctx, NormGradArgs a, float *grad_weight, hipStream_t s) {
-    const RowShape sh = row_shape(a.dim, Vec<T>::kLen);
+    const RowShape sh = row_shape(a.dim, Vec<T>::kLen, a.cap_rows);
     const int threads = std::max(sh.lanes, kBlock);
-    const int grid = static_cast<int>(std::min<int64_t>(ceil_div(a.cap_rows, threads / sh.lanes), sh.lanes > kBlock ? kNormParts / 2 : kNormParts));
+    const int grid = static_cast<int>(std::min<int64_t>(ceil_div(a.cap_rows, threads / sh.lanes), kNormParts));
+    const bool past = a.cap_rows * a.dim * (a.grad_sum ? 4 : 3) * int64_t(sizeof(T)) >= kPastBytes;
     if (grad_weight) {
         int rc = ensure_layer_scratch(ctx, norm_scratch_bytes(a.dim), s, "mqg_rms_norm_backward");
         if (rc != MQG_OK) return rc;
         a.parts = reinterpret_cast<float *>(ctx->layer_scratch);
     }
-#define MQG_GO(T, L, N) MQG_LAUNCH(ctx, "k_rms_norm_backward", s, (k_rms_norm_backward<T, L, N><<<grid, threads, 0, s>>>(a)))
+#define MQG_GO(T, L, N)                                                                                                        \
+    do {                                                                                                                       \
+        if (past) MQG_LAUNCH(ctx, "k_rms_norm_backward", s, (k_rms_norm_backward<T, L, N, true><<<grid, threads, 0, s>>>(a)));      \
+        else MQG_LAUNCH(ctx, "k_rms_norm_backward", s, (k_rms_norm_backward<T, L, N, false><<<grid, threads, 0, s>>>(a)));          \
+    } while (0)
     if (grid > 0) {
         MQG_NORM_SHAPES(T, MQG_GO)
     }
 #undef MQG_GO
     if (grad_weight)
         MQG_LAUNCH(ctx, "k_sum_parts", s,
-                   (k_sum_parts<<<static_cast<int>(ceil_div(a.dim, kSumCols)), kBlock, 0, s>>>(a.parts, grid, a.dim, grad_weight)));
+                   (k_sum_parts<<<static_cast<int>(ceil_div(a.dim, kSumCols)), kSumThreads, 0, s>>>(a.parts, grid, a.dim, grad_weight)));
     return MQG_OK;
 }
 #undef MQG_NORM_SHAPES
