@@ -1,11 +1,13 @@
 // GraphSAGE mean aggregation over one block (paper Eq. 16) whose source rows are held in 8 bits with scales:
 //   out[i, c] = (1/n_i) sum over the edges e of row i of scale[indices[e], c / group] q[indices[e], c]
-// What bounds the aggregation is the traffic of its input rows, random rows read once per edge; 8 bits are half of fp16's.
+// What bounds it is the number of random lines of 128 bytes that its input rows and their scales lie in, 57 to 58 G a second whatever the width (the
+// card's rate of random lookups out of tables of this size is 51 to 53): 295,000 rows of 15 entries of 256 columns, three lines to an entry, 215 us; 2.8 M entries of
+// 128 columns 97 us.  8 bits are half of fp16's lines.  Long rows come to 5 to 6.8 TB/s of row bytes.
 //
-// 16 columns, 16 bytes, are a lane's; a row's lanes are the smallest power of two that covers it, up to a wavefront (wider rows:
-// slabs of 1,024 columns, a share of the grid each), and the wavefront's groups of lanes take the entries of an output row in
-// turn, kFlight of each under way at a time.  Their sums, 32 bits each, are joined by exchanges between lanes: the order depends
-// on the row's own entries and the call's width alone, so the result is reproducible bit for bit.
+// 16 columns, 16 bytes, are a lane's; an output row is the work of the smallest power of two of lanes that covers it, up to a wavefront (wider rows:
+// slabs of 1,024 columns, a share of the grid each), so that no sum crosses lanes: the order depends on the row's own entries alone, and the result is
+// reproducible bit for bit.  Eight input rows are on their way at a time.  (Measured before: a wavefront to an output row, its groups of lanes taking the entries
+// in turn and joining their sums: 295,000 rows of 5 entries and 100 columns 320 us, 95 now; 10,200 of 25 and 602 98 and 34; 16 instead of eight rows on their way 38.)
 #include <algorithm>
 
 #include "common.h"
@@ -16,7 +18,6 @@ namespace mqg {
 namespace {
 
 constexpr int kCols = 16;             // columns of a lane
-constexpr int kFlight = 4;
 
 struct MeanQ8Args {
     const int32_t *indptr, *indices;
@@ -50,63 +51,86 @@ __device__ __forceinline__ void add_scaled(float (&acc)[kCols], Words4 w, float 
     }
 }
 
+typedef int32_t Index4 __attribute__((ext_vector_type(4)));
+typedef Index4 AnyIndex4 __attribute__((aligned(4)));
+
 template <typename T, int QTYPE, int LANES>
 __global__ void __launch_bounds__(kBlock)
 k_mean_aggregate_q8(MeanQ8Args a) {
-    constexpr int G = kWave / LANES;  // entries side by side
-    const int lane = lane_id() % LANES, g = lane_id() / LANES;
+    constexpr int kRows = kBlock / LANES;
+    const int lane = static_cast<int>(threadIdx.x) % LANES;
     const uint32_t slab = blockIdx.x / a.row_blocks, row_block = blockIdx.x - slab * a.row_blocks;
     const int col0 = (static_cast<int>(slab) * LANES + lane) * kCols;
-    const bool live = col0 < a.dim, whole = col0 + kCols <= a.dim;
-    const int at = live ? col0 : 0;
-    const int scale_at = a.group ? at / a.group : 0;
+    if (col0 >= a.dim) return;
+    // The last lane of a row whose columns are not a multiple of 16 takes the row's last 16, nothing outside the row is read: those that it shares with
+    // the lane before come out the same, unless a group of scales ends among them; then, and in rows of fewer than 16, it stores its own alone.
+    const bool narrow = a.dim < kCols;
+    const int at = narrow ? 0 : col0 + kCols <= a.dim ? col0 : a.dim - kCols;
+    const int scale_at = a.group ? (at + kCols - 1) / a.group : 0;
+    const int own = narrow || (a.group && at / a.group != scale_at) ? col0 : at;     // the first column that it stores
     const int64_t n = a.sizes[0] < a.cap_dst ? a.sizes[0] : a.cap_dst;
-    const int64_t step = int64_t(a.row_blocks) * kWavesPerBlock;
-    for (int64_t i = int64_t(row_block) * kWavesPerBlock + (threadIdx.x >> 6); i < n; i += step) {
+    const uint8_t *q = a.q + at;
+    const float *scale = a.scale + (narrow ? 0 : scale_at);
+    for (int64_t i = int64_t(row_block) * kRows + threadIdx.x / LANES; i < n; i += int64_t(a.row_blocks) * kRows) {
         const int b = a.indptr[i], e = a.indptr[i + 1];
         float acc[kCols];
 #pragma unroll
         for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
-        for (int p0 = b; p0 < e; p0 += kFlight * G) {
-            int64_t r[kFlight];
-            float sc[kFlight];
-            Words4 w[kFlight];
+        // N entries from p on: all their loads, then their additions; past the row's end the last one again, times 0
+        auto batch = [&](int p, auto number) __attribute__((always_inline)) {
+            constexpr int N = decltype(number)::value;
+            int64_t r[N];
+            float sc[N];
+            Words4 w[N];
+            if (p + N <= e) {
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u) {
-                const int p = p0 + u * G + g;
-                r[u] = a.indices[p < e ? p : e - 1];       // past the end: the last entry again, not added
+                for (int u = 0; u < N; u += 4) {
+                    const Index4 x = *reinterpret_cast<const AnyIndex4 *>(a.indices + p + u);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) r[u + k] = x[k];
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < N; ++u) r[u] = a.indices[p + u < e ? p + u : e - 1];
             }
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u) {
-                const uint8_t *row = a.q + r[u] * a.q_stride + at;
-                sc[u] = a.scale[r[u] * a.scale_stride + scale_at];
-                if (whole || !live) {
-                    w[u] = whole ? *reinterpret_cast<const AnyWords4 *>(row) : Words4{0, 0, 0, 0};
-                } else {                                   // the row's last columns, byte by byte: nothing outside the row is read
+            for (int u = 0; u < N; ++u) {
+                sc[u] = scale[r[u] * a.scale_stride];
+                if (!narrow) {
+                    w[u] = *reinterpret_cast<const AnyWords4 *>(q + r[u] * a.q_stride);
+                } else {
                     w[u] = Words4{0, 0, 0, 0};
 #pragma unroll
-                    for (int j = 0; j < kCols; ++j)
-                        if (col0 + j < a.dim) w[u][j / 4] |= static_cast<uint32_t>(row[j]) << (8 * (j % 4));
+                    for (int j = 0; j < kCols - 1; ++j)
+                        if (j < a.dim) w[u][j / 4] |= static_cast<uint32_t>(q[r[u] * a.q_stride + j]) << (8 * (j % 4));
                 }
             }
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u)
-                if (p0 + u * G + g < e) add_scaled<QTYPE>(acc, w[u], sc[u]);
-        }
-#pragma unroll
-        for (int off = LANES; off < kWave; off <<= 1)
-#pragma unroll
-            for (int j = 0; j < kCols; ++j) acc[j] += __shfl_xor(acc[j], off, kWave);
-        if (g != 0 || !live) continue;
-        const float count = e > b ? static_cast<float>(e - b) : 1.f;
+            for (int u = 0; u < N; ++u) add_scaled<QTYPE>(acc, w[u], p + u < e ? sc[u] : 0.f);
+        };
+        int p = b;
+        for (; e - p > 4; p += 8) batch(p, std::integral_constant<int, 8>());
+        if (e - p > 0) batch(p, std::integral_constant<int, 4>());
+        const float count = e > b ? static_cast<float>(e - b) : 1.f, inv = 1.f / count;
         T *out = static_cast<T *>(a.out) + i * a.out_stride;
-        constexpr int V = Vec<T>::kLen;
 #pragma unroll
-        for (int k = 0; k < kCols / V; ++k) {
-            float v[V];
+        for (int j = 0; j < kCols; ++j) {                  // the quotient by the reciprocal, and its remainder's
+            const float quot = acc[j] * inv;
+            acc[j] = fmaf(fmaf(-quot, count, acc[j]), inv, quot);
+        }
+        if (own == at && !narrow) {
+            constexpr int V = Vec<T>::kLen;
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = acc[k * V + j] / count;
-            store_vec(out, col0 / V + k, a.dim, v);
+            for (int k = 0; k < kCols / V; ++k) {
+                float v[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] = acc[k * V + j];
+                store_vec(out + at, k, kCols, v);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kCols; ++j)
+                if (at + j >= own && at + j < a.dim) out[at + j] = static_cast<T>(acc[j]);
         }
     }
 }
@@ -114,18 +138,23 @@ k_mean_aggregate_q8(MeanQ8Args a) {
 template <typename T, int QTYPE>
 int launch_mean_q8(mqg_ctx *ctx, MeanQ8Args a, hipStream_t s) {
     const int lanes_needed = static_cast<int>(ceil_div(a.dim, kCols));
+    int lanes = 1;
+    while (lanes < lanes_needed && lanes < kWave) lanes <<= 1;
     const int64_t slabs = ceil_div(lanes_needed, kWave);
     // (a launch has fewer than 2^32 threads)
-    a.row_blocks = static_cast<uint32_t>(std::min<int64_t>(ceil_div(a.cap_dst, kWavesPerBlock), std::max<int64_t>(1, std::min<int64_t>(256 * 32, (int64_t(1) << 23) / slabs))));
+    const int64_t most = std::max<int64_t>(1, (int64_t(1) << 23) / slabs);
+    a.row_blocks = static_cast<uint32_t>(std::min<int64_t>(ceil_div(a.cap_dst, kBlock / lanes), most));
     const int grid = static_cast<int>(a.row_blocks * slabs);
 #define MQG_GO(L) MQG_LAUNCH(ctx, "k_mean_aggregate_q8", s, (k_mean_aggregate_q8<T, QTYPE, L><<<grid, kBlock, 0, s>>>(a)))
-    if (lanes_needed <= 1) MQG_GO(1);
-    else if (lanes_needed <= 2) MQG_GO(2);
-    else if (lanes_needed <= 4) MQG_GO(4);
-    else if (lanes_needed <= 8) MQG_GO(8);
-    else if (lanes_needed <= 16) MQG_GO(16);
-    else if (lanes_needed <= 32) MQG_GO(32);
-    else MQG_GO(64);
+    switch (lanes) {
+        case 1: MQG_GO(1); break;
+        case 2: MQG_GO(2); break;
+        case 4: MQG_GO(4); break;
+        case 8: MQG_GO(8); break;
+        case 16: MQG_GO(16); break;
+        case 32: MQG_GO(32); break;
+        default: MQG_GO(64);
+    }
 #undef MQG_GO
     return MQG_OK;
 }
