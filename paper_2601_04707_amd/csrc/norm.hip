@@ -94,33 +94,48 @@ struct RowLanes {
     }
 };
 
-// The scale of a group whose largest |y| has the bit pattern `most` (patterns of absolute values order as the values do, with infinity and NaN
-// above all others: a group that holds one has the scale NaN, so that all its values read NaN).
-__device__ __forceinline__ float scale_of(uint32_t most, float top) {
-    if (most >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
-    const float s = __uint_as_float(most) / top;
-    return s > 0x1p-126f ? s : 0x1p-126f;
+// How a group is taken to 8 bits, from z = s w and the row's r, y = z r.  Values and scale have r in common, so q = z / (max|z| / top) has two roundings before
+// its own and r's is none of them; where that quotient would leave 32 bits' range, or the scale is the least one, q = y / scale.
+// most: the largest |z|'s bit pattern (patterns of absolute values order as the values do, with infinity and NaN above all others): a group that
+// holds a value that is not finite has the scale NaN, so that all its values read NaN.
+struct Scale {
+    float scale, by, div;             // q = (z by) / div
+};
+__device__ __forceinline__ Scale scale_of(uint32_t most, float r, float top) {
+    const float t = __uint_as_float(most) / top, scale = t * r;
+    if (!(scale < __uint_as_float(0x7F800000u))) {
+        const float nan = __uint_as_float(0x7FC00000u);
+        return {nan, nan, nan};
+    }
+    if (!(scale > 0x1p-126f)) return {0x1p-126f, r, 0x1p-126f};
+    return t > 0x1p-100f ? Scale{scale, 1.f, t} : Scale{scale, r, scale};
 }
 
-// V values of a row divided by their scale, in 8 bits
+// V values of a row in 8 bits
 template <int V>
-__device__ __forceinline__ void store_q(uint8_t *row, int i, int dim, const float (&y)[V], float scale, int q_type) {
-    const float inv = 1.0f / scale;
+__device__ __forceinline__ void store_q(uint8_t *row, int i, int dim, const float (&z)[V], const Scale &s, int q_type) {
+    const float inv = 1.0f / s.div;
+    float y[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {                          // the quotient by the reciprocal, and its remainder's
+        const float num = z[j] * s.by, quot = num * inv;
+        y[j] = fmaf(fmaf(-quot, s.div, num), inv, quot);
+    }
     uint32_t w[V / 4];
     if (q_type == MQG_Q_E4M3) {
 #pragma unroll
         for (int k = 0; k < V / 4; ++k) {
-            int p = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k] * inv, y[4 * k + 1] * inv, 0, false);
-            w[k] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2] * inv, y[4 * k + 3] * inv, p, true));
+            int p = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k], y[4 * k + 1], 0, false);
+            w[k] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2], y[4 * k + 3], p, true));
         }
     } else {
-        const bool number = scale == scale;
+        const bool number = s.scale == s.scale;
 #pragma unroll
         for (int k = 0; k < V / 4; ++k) {
             w[k] = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int v = number ? static_cast<int>(rintf(y[4 * k + j] * inv)) : 0;
+                const int v = number ? static_cast<int>(rintf(y[4 * k + j])) : 0;
                 w[k] |= (static_cast<uint32_t>(v) & 0xFFu) << (8 * j);
             }
         }
@@ -191,11 +206,16 @@ k_rms_norm(NormArgs a) {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int j = 0; j < V; ++j) s[k][j] = s[k][j] * r * w[k][j];
+            for (int j = 0; j < V; ++j) s[k][j] *= w[k][j];
         if (a.y) {
             T *y = static_cast<T *>(a.y) + row * a.y_stride;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) store_vec<PAST>(y, k * LANES + lane, dim, s[k]);
+            for (int k = 0; k < NV; ++k) {
+                float v[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] = s[k][j] * r;
+                store_vec<PAST>(y, k * LANES + lane, dim, v);
+            }
         }
         if (!a.q) continue;
         uint8_t *q = a.q + row * a.q_stride;
@@ -211,17 +231,17 @@ k_rms_norm(NormArgs a) {
             uint32_t m = most[0];
 #pragma unroll
             for (int k = 1; k < NV; ++k) m = max_u32(m, most[k]);
-            const float sc = scale_of(lanes.max(m), top);
-            if (lane == 0) scale[0] = sc;
+            const Scale sc = scale_of(lanes.max(m), r, top);
+            if (lane == 0) scale[0] = sc.scale;
 #pragma unroll
             for (int k = 0; k < NV; ++k) store_q(q, k * LANES + lane, dim, s[k], sc, a.q_type);
         } else {
             const int width = group_lanes < LANES ? group_lanes : LANES;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                const float sc = scale_of(lanes_max(most[k], width), top);
+                const Scale sc = scale_of(lanes_max(most[k], width), r, top);
                 const int i = k * LANES + lane;
-                if (lane % width == 0 && i * V < dim) scale[i / group_lanes] = sc;
+                if (lane % width == 0 && i * V < dim) scale[i / group_lanes] = sc.scale;
                 store_q(q, i, dim, s[k], sc, a.q_type);
             }
         }

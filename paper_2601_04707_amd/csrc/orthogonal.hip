@@ -224,11 +224,39 @@ static_assert(kBand == 8, "the counts of tiles before a band are written out");
 
 // The epilogue of one block of the product, 32 x 32, whose sums lie in LDS as the matrix instruction leaves them, register e of lane l at
 // e * kAccRow + l: row 8 (e / 4) + 4 (l / 32) + e % 4, column l % 32.  PARTS of them, part_len apart, are added; the finished values go back to the
-// first, from which they are stored turned.  `threads` threads, t among them; sync() orders LDS between them.
+// first, from which they are stored turned.  THREADS threads, t among them, have 128 chunks of eight columns of a row; sync() orders LDS between them.
 constexpr int kAccRow = kWave + 4;    // (16 rows of a column in other banks)
 constexpr int kAccLen = 16 * kAccRow;
-template <int EPI, int PARTS, typename Sync>
-__device__ __forceinline__ void finish_block(const ProductArgs &a, float *acc, int part_len, int mat, int mb, int nb, bool mirror, int t, int threads, Sync sync) {
+template <int EPI>
+__device__ __forceinline__ int unit_row(int u) { return EPI == kOut ? u >> 2 : u % kSide; }        // the output is written along its rows, four threads to each
+template <int EPI>
+__device__ __forceinline__ int unit_chunk(int u) { return EPI == kOut ? u & 3 : u / kSide; }
+
+// What the epilogue adds, on its way before the sums are there
+template <int THREADS>
+struct Own {
+    static constexpr int kEach = THREADS < 128 ? 128 / THREADS : 1;
+    Half8 hi[kEach], lo[kEach];
+};
+template <int EPI, int THREADS>
+__device__ __forceinline__ Own<THREADS> load_own(const ProductArgs &a, int mat, int mb, int nb, int t) {
+    Own<THREADS> own;
+    if constexpr (EPI != kGram) {
+#pragma unroll
+        for (int k = 0; k < own.kEach; ++k) {
+            const int u = t + k * THREADS < 128 ? t + k * THREADS : 0;
+            const F16 *from = a.own + mat * a.own_mat + (int64_t(mb) * (a.n / kSide) + nb) * kBlockLen + chunk_at(unit_row<EPI>(u), unit_chunk<EPI>(u));
+            own.hi[k] = *reinterpret_cast<const Half8 *>(from);
+            own.lo[k] = *reinterpret_cast<const Half8 *>(from + kTermLen);
+        }
+    }
+    return own;
+}
+
+template <int EPI, int PARTS, int THREADS, typename Sync>
+__device__ __forceinline__ void finish_block(const ProductArgs &a, const Own<THREADS> &own, float *acc, int part_len, int mat, int mb, int nb, bool mirror, int t,
+                                             Sync sync) {
+    constexpr int N = Own<THREADS>::kEach;
     auto store = [&](const float (&v)[8], F16 *to) __attribute__((always_inline)) {
         Half8 hi, lo;
 #pragma unroll
@@ -241,71 +269,83 @@ __device__ __forceinline__ void finish_block(const ProductArgs &a, float *acc, i
         *reinterpret_cast<Half8 *>(to) = hi;
         *reinterpret_cast<Half8 *>(to + kTermLen) = lo;
     };
-    const int64_t block = (int64_t(mb) * (a.n / kSide) + nb) * kBlockLen, block_turned = (int64_t(nb) * (a.m / kSide) + mb) * kBlockLen;
-    for (int u = t; u < 128; u += threads) {               // eight columns of a row; the output is written along its rows, four threads to each
-        const int r = EPI == kOut ? u >> 2 : u % kSide, c = EPI == kOut ? u & 3 : u / kSide;
+    const bool mine = THREADS <= 128 || t < 128;
+    float v[N][8];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        if (!mine) break;
+        const int u = t + k * THREADS, r = unit_row<EPI>(u), c = unit_chunk<EPI>(u);
         float *at = acc + ((r >> 3) * 4 + (r & 3)) * kAccRow + 32 * ((r >> 2) & 1) + 8 * c;
-        Half8 own_hi, own_lo;
-        if constexpr (EPI != kGram) {
-            const F16 *own = a.own + mat * a.own_mat + block + chunk_at(r, c);
-            own_hi = *reinterpret_cast<const Half8 *>(own);
-            own_lo = *reinterpret_cast<const Half8 *>(own + kTermLen);
-        }
         Float4 x{0, 0, 0, 0}, y{0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < PARTS; ++k) {
-            x += *reinterpret_cast<const Float4 *>(at + k * part_len);
-            y += *reinterpret_cast<const Float4 *>(at + k * part_len + 4);
+        for (int p = 0; p < PARTS; ++p) {
+            x += *reinterpret_cast<const Float4 *>(at + p * part_len);
+            y += *reinterpret_cast<const Float4 *>(at + p * part_len + 4);
         }
-        float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            v[j] = (j < 4 ? x[j % 4] : y[j % 4]) * a.acc_by;
-            if constexpr (EPI != kGram) v[j] += a.own_by * (static_cast<float>(own_hi[j]) + static_cast<float>(own_lo[j]));
+            v[k][j] = (j < 4 ? x[j % 4] : y[j % 4]) * a.acc_by;
+            // (as one operation: the compiler would choose which product to round, and not in all kernels the same)
+            if constexpr (EPI != kGram) v[k][j] = fmaf(a.own_by, static_cast<float>(own.hi[k][j]) + static_cast<float>(own.lo[k][j]), v[k][j]);
         }
-        if constexpr (EPI != kOut) {
-            store(v, a.to + mat * a.to_mat + block + chunk_at(r, c));
-            if (EPI == kIterate || mirror) {
-                *reinterpret_cast<Float4 *>(at) = Float4{v[0], v[1], v[2], v[3]};
-                *reinterpret_cast<Float4 *>(at + 4) = Float4{v[4], v[5], v[6], v[7]};
-            }
-        } else {
-            const int row = mb * kSide + r, col0 = nb * kSide + 8 * c;
-            if (row >= a.out_m) continue;
-            const int64_t to = mat * a.out_mat + row * a.out_row;
-            if (a.step) {
-                float *w = static_cast<float *>(a.out) + to;
+        if (EPI == kIterate || (EPI != kOut && mirror)) {
+            *reinterpret_cast<Float4 *>(at) = Float4{v[k][0], v[k][1], v[k][2], v[k][3]};
+            *reinterpret_cast<Float4 *>(at + 4) = Float4{v[k][4], v[k][5], v[k][6], v[k][7]};
+        }
+    }
+    if constexpr (EPI == kOut) {
+        if (a.step) {                                      // all weights are on their way before the first is written
+            float w[N][2][4];
+            auto each = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (col0 + 4 * h >= a.out_n) continue;
-                    float z[4];
-                    load_vec(w, col0 / 4 + h, a.out_n, z);
+                for (int k = 0; k < N; ++k) {
+                    const int u = t + k * THREADS, row = mb * kSide + unit_row<EPI>(u), col0 = nb * kSide + 8 * unit_chunk<EPI>(u);
+                    if (!mine || row >= a.out_m) continue;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) z[j] = a.keep * z[j] + v[4 * h + j];
-                    store_vec(w, col0 / 4 + h, a.out_n, z);
+                    for (int h = 0; h < 2; ++h)
+                        if (col0 + 4 * h < a.out_n) f(static_cast<float *>(a.out) + mat * a.out_mat + row * a.out_row, col0 / 4 + h, k, h);
                 }
-            } else if (a.out_type == MQG_F16) {
-                store_vec(static_cast<F16 *>(a.out) + to, col0 / 8, a.out_n, v);
+            };
+            each([&](const float *at, int i, int k, int h) __attribute__((always_inline)) { load_vec(at, i, a.out_n, w[k][h]); });
+            each([&](float *at, int i, int k, int h) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[k][h][j] = fmaf(a.keep, w[k][h][j], v[k][4 * h + j]);
+                store_vec(at, i, a.out_n, w[k][h]);
+            });
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int u = t + k * THREADS, row = mb * kSide + unit_row<EPI>(u), col0 = nb * kSide + 8 * unit_chunk<EPI>(u);
+            if (!mine || row >= a.out_m) continue;
+            const int64_t to = mat * a.out_mat + row * a.out_row;
+            if (a.out_type == MQG_F16) {
+                store_vec(static_cast<F16 *>(a.out) + to, col0 / 8, a.out_n, v[k]);
             } else if (a.out_type == MQG_BF16) {
-                store_vec(static_cast<BF16 *>(a.out) + to, col0 / 8, a.out_n, v);
+                store_vec(static_cast<BF16 *>(a.out) + to, col0 / 8, a.out_n, v[k]);
             } else {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float z[4] = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+                    const float z[4] = {v[k][4 * h], v[k][4 * h + 1], v[k][4 * h + 2], v[k][4 * h + 3]};
                     store_vec(static_cast<float *>(a.out) + to, col0 / 4 + h, a.out_n, z);
                 }
             }
         }
-    }
-    if constexpr (EPI != kOut) {
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int u = t + k * THREADS;
+            if (mine) store(v[k], a.to + mat * a.to_mat + (int64_t(mb) * (a.n / kSide) + nb) * kBlockLen + chunk_at(unit_row<EPI>(u), unit_chunk<EPI>(u)));
+        }
         if (EPI != kIterate && !mirror) return;            // (the same in all threads of a tile)
         sync();
-        for (int u = t; u < 128; u += threads) {           // eight rows of a column
-            const int col = u % kSide, c = u / kSide;
-            float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = acc[(c * 4 + (j & 3)) * kAccRow + col + 32 * (j >> 2)];
-            store(v, a.to_turned + mat * a.to_mat + block_turned + chunk_at(col, c));
+        for (int k = 0; k < N; ++k) {                      // eight rows of a column
+            const int u = t + k * THREADS, col = u % kSide, c = u / kSide;
+            if (!mine) break;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[k][j] = acc[(c * 4 + (j & 3)) * kAccRow + col + 32 * (j >> 2)];
+            store(v[k], a.to_turned + mat * a.to_mat + (int64_t(nb) * (a.m / kSide) + mb) * kBlockLen + chunk_at(col, c));
         }
     }
 }
@@ -376,20 +416,23 @@ k_orth_product(ProductArgs a) {
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");     // the stages are free
     float *mine = reinterpret_cast<float *>(lds) + wave * kAccLen;
+    const int mb = tile.m * BM + wm, nb = tile.n * BN + wn;
+    Own<kWave> next = load_own<EPI, kWave>(a, tile.mat, mb, nb, lane);
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int b = 0; b < FM * FN; ++b) {
+        const int i = b / FN, j = b % FN;
+        const Own<kWave> own = next;
+        if (b + 1 < FM * FN) next = load_own<EPI, kWave>(a, tile.mat, mb + (b + 1) / FN, nb + (b + 1) % FN, lane);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) mine[e * kAccRow + lane] = acc[i][j][e];
-            wave_lds_sync();
-            finish_block<EPI, 1>(a, mine, 0, tile.mat, tile.m * BM + wm + i, tile.n * BN + wn + j, tile.m != tile.n, lane, kWave, [] { wave_lds_sync(); });
-            wave_lds_sync();
-        }
+        for (int e = 0; e < 16; ++e) mine[e * kAccRow + lane] = acc[i][j][e];
+        wave_lds_sync();
+        finish_block<EPI, 1, kWave>(a, own, mine, 0, tile.mat, mb + i, nb + j, tile.m != tile.n, lane, [] { wave_lds_sync(); });
+        wave_lds_sync();
+    }
 }
 
 // The same for few tiles: F x F blocks of the product to a workgroup, whose depth eight wavefronts share.  Each takes every eighth block of P
-// and of Q, from memory to registers, AHEAD of them on their way together, and the eight sums are added in LDS.
+// and of Q, from memory to registers, AHEAD of them on their way together, and their sums are added in LDS.  (Sixteen: no faster.)
 // SUB > 1: the blocks of the tiles of SUB x SUB blocks from number first_tile on.
 constexpr int kFewWaves = 8;
 template <int EPI, int SUB, int F, int AHEAD>
@@ -447,6 +490,9 @@ k_orth_product_few(ProductArgs a) {
     for (; left >= AHEAD; left -= AHEAD, line += AHEAD * kFewWaves) batch(line, integral_constant<int, AHEAD>());
     if (AHEAD > 2 && left == 2) batch(line, integral_constant<int, 2>());
     if (left == 1) batch(line, integral_constant<int, 1>());
+    constexpr int kThreads = kFewWaves * kWave / (F * F);  // to a block
+    const int b = static_cast<int>(threadIdx.x) / kThreads, mb = tile.m * F + b / F, nb = tile.n * F + b % F;
+    const Own<kThreads> own = load_own<EPI, kThreads>(a, tile.mat, mb, nb, static_cast<int>(threadIdx.x) % kThreads);
 #pragma unroll
     for (int i = 0; i < F; ++i)
 #pragma unroll
@@ -454,13 +500,40 @@ k_orth_product_few(ProductArgs a) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) lds[(wave * F * F + i * F + j) * kAccLen + e * kAccRow + lane] = acc[i][j][e];
     __syncthreads();
-    constexpr int kThreads = kFewWaves * kWave / (F * F);  // to a block
-    const int b = static_cast<int>(threadIdx.x) / kThreads;
-    finish_block<EPI, kFewWaves>(a, lds + b * kAccLen, F * F * kAccLen, tile.mat, tile.m * F + b / F, tile.n * F + b % F, mirror,
-                                 static_cast<int>(threadIdx.x) % kThreads, kThreads, [] { __syncthreads(); });
+    finish_block<EPI, kFewWaves, kThreads>(a, own, lds + b * kAccLen, F * F * kAccLen, tile.mat, mb, nb, mirror, static_cast<int>(threadIdx.x) % kThreads,
+                                           [] { __syncthreads(); });
 }
 
 // ---------------------------------------------------------------- small matrices
+
+// What the matrix instruction leaves in a lane are four times four neighbouring values of a column: half of chunk c of row lane % 32 of the block turned.
+__device__ __forceinline__ int turned_at(int lane, int c) { return chunk_at(lane & 31, c) + 4 * (lane >> 5); }
+__device__ __forceinline__ void store_turned(F16 *block, int lane, const Float16v &v) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        Half4 hi, lo;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            F16 h, l;
+            split(v[4 * c + j], &h, &l);
+            hi[j] = h;
+            lo[j] = l;
+        }
+        F16 *to = block + turned_at(lane, c);
+        *reinterpret_cast<Half4 *>(to) = hi;
+        *reinterpret_cast<Half4 *>(to + kTermLen) = lo;
+    }
+}
+// v <- by v + own_by (the block turned)
+__device__ __forceinline__ void add_turned(Float16v &v, float by, const F16 *block, int lane, float own_by) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const F16 *own = block + turned_at(lane, c);
+        const Half4 hi = *reinterpret_cast<const Half4 *>(own), lo = *reinterpret_cast<const Half4 *>(own + kTermLen);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[4 * c + j] = fmaf(own_by, static_cast<float>(hi[j]) + static_cast<float>(lo[j]), by * v[4 * c + j]);
+    }
+}
 
 // What the three products of a step multiply their sums and their own values by
 struct StepScales {
@@ -630,31 +703,6 @@ k_orth_small(SmallArgs a) {
         }
         return acc;
     };
-    // Registers 4 c ... 4 c + 3 of a lane are four neighbouring values, half of chunk c, of row lane % 32 of the block turned
-    auto turned_at = [&](F16 *block, int c) __attribute__((always_inline)) { return block + chunk_at(own_lane & 31, c) + 4 * (own_lane >> 5); };
-    auto store_turned = [&](F16 *block, const Float16v &v) __attribute__((always_inline)) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            Half4 hi, lo;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                F16 h, l;
-                split(v[4 * c + j], &h, &l);
-                hi[j] = h;
-                lo[j] = l;
-            }
-            *reinterpret_cast<Half4 *>(turned_at(block, c)) = hi;
-            *reinterpret_cast<Half4 *>(turned_at(block, c) + kTermLen) = lo;
-        }
-    };
-    auto add_own = [&](Float16v &v, float by, F16 *block, float own_by) __attribute__((always_inline)) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const Half4 hi = *reinterpret_cast<const Half4 *>(turned_at(block, c)), lo = *reinterpret_cast<const Half4 *>(turned_at(block, c) + kTermLen);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[4 * c + j] = by * v[4 * c + j] + own_by * (static_cast<float>(hi[j]) + static_cast<float>(lo[j]));
-        }
-    };
     Float16v v[kIterateEach];
 #pragma unroll 1
     for (int s = 0;; ++s) {
@@ -664,7 +712,7 @@ k_orth_small(SmallArgs a) {
             const int i = b / nb, j = b % nb;
             Float16v g = product(x + i * kb * kBlockLen, x + j * kb * kBlockLen, kb);
             g *= by.gram;
-            store_turned(gram + (j * nb + i) * kBlockLen, g);
+            store_turned(gram + (j * nb + i) * kBlockLen, own_lane, g);
         }
         __syncthreads();
 #pragma unroll
@@ -672,13 +720,13 @@ k_orth_small(SmallArgs a) {
             const int b = wave + e * kSmallWaves, i = b / nb, j = b % nb;
             if (b >= nb * nb) continue;
             v[e] = product(gram + i * nb * kBlockLen, gram + j * nb * kBlockLen, nb);
-            add_own(v[e], by.poly, gram + (j * nb + i) * kBlockLen, by.poly_own);
+            add_turned(v[e], by.poly, gram + (j * nb + i) * kBlockLen, own_lane, by.poly_own);
         }
         __syncthreads();                                   // B in the place of G
 #pragma unroll
         for (int e = 0; e < kGramEach; ++e) {
             const int b = wave + e * kSmallWaves;
-            if (b < nb * nb) store_turned(gram + (b % nb * nb + b / nb) * kBlockLen, v[e]);
+            if (b < nb * nb) store_turned(gram + (b % nb * nb + b / nb) * kBlockLen, own_lane, v[e]);
         }
         __syncthreads();
 #pragma unroll
@@ -686,7 +734,7 @@ k_orth_small(SmallArgs a) {
             const int b = wave + e * kSmallWaves, i = b / kb, j = b % kb;
             if (b >= nb * kb) continue;
             v[e] = product(gram + i * nb * kBlockLen, xt + j * nb * kBlockLen, nb);
-            add_own(v[e], by.x, xt + (j * nb + i) * kBlockLen, by.x_own);
+            add_turned(v[e], by.x, xt + (j * nb + i) * kBlockLen, own_lane, by.x_own);
         }
         if (s + 1 == a.steps) break;
         __syncthreads();
@@ -694,7 +742,7 @@ k_orth_small(SmallArgs a) {
         for (int e = 0; e < kIterateEach; ++e) {
             const int b = wave + e * kSmallWaves, i = b / kb, j = b % kb;
             if (b >= nb * kb) continue;
-            store_turned(xt + (j * nb + i) * kBlockLen, v[e]);
+            store_turned(xt + (j * nb + i) * kBlockLen, own_lane, v[e]);
             // as it lies: four lanes exchange their four rows of a column each for a row of four columns each
             F16 *block = x + b * kBlockLen + chunk_at(4 * (own_lane >> 5) + (own_lane & 3), (own_lane & 31) / 8) + (own_lane & 4);
 #pragma unroll
@@ -727,7 +775,7 @@ k_orth_small(SmallArgs a) {
             const int64_t at = mat * a.out_mat + r * a.out_row + c;
             if (a.step) {
                 float *w = static_cast<float *>(a.out) + at;
-                *w = a.keep * *w + v[e][k];
+                *w = fmaf(a.keep, *w, v[e][k]);
             } else if (a.out_type == MQG_F16) {
                 static_cast<F16 *>(a.out)[at] = static_cast<F16>(v[e][k]);
             } else if (a.out_type == MQG_BF16) {
@@ -959,9 +1007,8 @@ int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
         a.to_turned = tall ? x : then;
         a.m = static_cast<int32_t>(tall ? l.k : l.n);
         a.n = static_cast<int32_t>(tall ? l.n : l.k);
-        if (i + 1 < call.steps) {
-            rc = launch_product<kIterate>(ctx, a, mats, l.x_kernel, s);
-        } else {
+        const bool last = i + 1 == call.steps;
+        if (last) {
             a.out = call.out;
             a.out_row = call.out_row;
             a.out_mat = call.out_mat;
@@ -970,8 +1017,8 @@ int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
             a.out_type = call.out_type;
             a.step = call.step;
             a.keep = call.keep;
-            rc = launch_product<kOut>(ctx, a, mats, l.x_kernel, s);
         }
+        rc = last ? launch_product<kOut>(ctx, a, mats, l.x_kernel, s) : launch_product<kIterate>(ctx, a, mats, l.x_kernel, s);
         if (rc != MQG_OK) return rc;
     }
     return MQG_OK;

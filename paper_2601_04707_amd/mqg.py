@@ -593,9 +593,10 @@ def mqg_weighted_aggregate_backward(ctx: Context, blocks: Blocks, l: int, edge_w
 
 def _rows(t: torch.Tensor, dtype, shape) -> int:
     """The row stride of a [rows, dim] tensor, checked."""
-    assert t.is_cuda and t.dtype == dtype and t.shape == shape, f"expected {tuple(shape)} of {dtype} on the GPU, got {tuple(t.shape)} of {t.dtype}"
-    assert t.stride(1) == 1 or shape[1] == 1
-    return t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
+    assert t.is_cuda and t.dtype is dtype and t.shape == shape, f"expected {tuple(shape)} of {dtype} on the GPU, got {tuple(t.shape)} of {t.dtype}"
+    row, col = t.stride()
+    assert col == 1 or shape[1] == 1
+    return row if shape[0] > 1 else max(row, shape[1])
 
 
 def _norm_inputs(weight, num_rows, dim):

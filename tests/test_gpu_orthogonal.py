@@ -281,3 +281,21 @@ def test_refusals(mqg, ctx):
     with pytest.raises(AssertionError):
         mqg.mqg_orthogonalize(ctx, u, u, steps=2, coeffs=[(1.5, -0.5, 0.0)] * 3)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("mats,rows,cols", [(1, 70, 900), (3, 900, 70), (1, 40, 700), (2, 700, 40), (1, 128, 4000), (1, 4000, 100), (40, 128, 1000), (9, 100, 130), (500, 20, 30),
+                                            (1, 1, 3000), (3, 100, 160), (1, 160, 96), (1, 1030, 1100), (3, 600, 1300), (1, 2200, 2200)])
+def test_matrices_by_every_kernel(mqg, ctx, mats, rows, cols, dtype):
+    """One launch, few rows or columns, single blocks, tiles of 64 and of 128 and the last tiles of a round."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(mats + rows * 7 + cols)
+    u = torch.randn((mats, rows, cols), generator=gen, device="cuda") + torch.randn((mats, rows, 3), generator=gen, device="cuda") @ torch.randn((mats, 3, cols), generator=gen, device="cuda")
+    u = u.to(dtype)
+    out = torch.full_like(u, 7.0)
+    mqg.mqg_orthogonalize(ctx, u, out, eps=EPS)
+    torch.cuda.synchronize()
+    for i in sorted({0, mats // 2, mats - 1}):
+        want, off = orth64(u[i], [USUAL] * 5)
+        err = float((out[i].double() - want).norm())
+        assert err <= off + UNIT[dtype] * float(want.norm()), (i, err, off)
