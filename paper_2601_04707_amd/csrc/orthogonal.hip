@@ -389,30 +389,42 @@ k_orth_product(ProductArgs a) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (line + 1 < deep) fetch(line + 1, (line + 1) & 1);
         const F16 *at = lds + (line & 1) * kStage + lane * 8;
+        Half8 ph[2][FM], pl[2][FM], qh[2][FN], ql[2][FN];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {                      // 16 values at a time
-            Half8 ph[FM], pl[FM], qh[FN], ql[FN];
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
                 const F16 *b = at + (wm + i) * kBlockLen + t * 512;
-                ph[i] = *reinterpret_cast<const Half8 *>(b);
-                pl[i] = *reinterpret_cast<const Half8 *>(b + kTermLen);
+                ph[t][i] = *reinterpret_cast<const Half8 *>(b);
+                pl[t][i] = *reinterpret_cast<const Half8 *>(b + kTermLen);
             }
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 const F16 *b = at + (BM + wn + j) * kBlockLen + t * 512;
-                qh[j] = *reinterpret_cast<const Half8 *>(b);
-                ql[j] = *reinterpret_cast<const Half8 *>(b + kTermLen);
+                qh[t][j] = *reinterpret_cast<const Half8 *>(b);
+                ql[t][j] = *reinterpret_cast<const Half8 *>(b + kTermLen);
             }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], qh[j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[t][i], ql[t][j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[t][i], qh[t][j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[t][i], qh[t][j], acc[i][j], 0, 0, 0);
                 }
+#ifndef NOSCHED
+        // the second half's reads between the first half's products
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * (FM + FN), 0);
+#pragma unroll
+        for (int k = 0; k < 2 * (FM + FN); ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x008, 6 * FM * FN - 2 * (FM + FN), 0);
+#endif
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");     // the stages are free
     float *mine = reinterpret_cast<float *>(lds) + wave * kAccLen;
