@@ -383,48 +383,51 @@ k_orth_product(ProductArgs a) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = Float16v{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     const int wm = wave / WN * FM, wn = wave % WN * FN;
+    struct Operands {                 // of 16 values
+        Half8 ph[FM], pl[FM], qh[FN], ql[FN];
+    };
+    auto read = [&](int stage, int t) __attribute__((always_inline)) {
+        const F16 *at = lds + stage * kStage + t * 512 + lane * 8;
+        Operands o;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            o.ph[i] = *reinterpret_cast<const Half8 *>(at + (wm + i) * kBlockLen);
+            o.pl[i] = *reinterpret_cast<const Half8 *>(at + (wm + i) * kBlockLen + kTermLen);
+        }
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            o.qh[j] = *reinterpret_cast<const Half8 *>(at + (BM + wn + j) * kBlockLen);
+            o.ql[j] = *reinterpret_cast<const Half8 *>(at + (BM + wn + j) * kBlockLen + kTermLen);
+        }
+        return o;
+    };
+    auto multiply = [&](const Operands &o) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.ph[i], o.ql[j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.pl[i], o.qh[j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.ph[i], o.qh[j], acc[i][j], 0, 0, 0);
+            }
+    };
+    constexpr int kReads = 2 * (FM + FN), kProducts = 3 * FM * FN;
     fetch(0, 0);
     for (int line = 0; line < deep; ++line) {
         // the line has arrived and this wavefront's reads of the other stage are done; behind the barrier that holds for all
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (line + 1 < deep) fetch(line + 1, (line + 1) & 1);
-        const F16 *at = lds + (line & 1) * kStage + lane * 8;
-        Half8 ph[2][FM], pl[2][FM], qh[2][FN], ql[2][FN];
+        const Operands first = read(line & 1, 0), second = read(line & 1, 1);
+        multiply(first);
+        multiply(second);
+        // the second half's reads between the first half's products, one and one
+        __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {                      // 16 values at a time
-#pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                const F16 *b = at + (wm + i) * kBlockLen + t * 512;
-                ph[t][i] = *reinterpret_cast<const Half8 *>(b);
-                pl[t][i] = *reinterpret_cast<const Half8 *>(b + kTermLen);
-            }
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const F16 *b = at + (BM + wn + j) * kBlockLen + t * 512;
-                qh[t][j] = *reinterpret_cast<const Half8 *>(b);
-                ql[t][j] = *reinterpret_cast<const Half8 *>(b + kTermLen);
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[t][i], ql[t][j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[t][i], qh[t][j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[t][i], qh[t][j], acc[i][j], 0, 0, 0);
-                }
-#ifndef NOSCHED
-        // the second half's reads between the first half's products
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * (FM + FN), 0);
-#pragma unroll
-        for (int k = 0; k < 2 * (FM + FN); ++k) {
+        for (int k = 0; k < kReads; ++k) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, 6 * FM * FN - 2 * (FM + FN), 0);
-#endif
+        __builtin_amdgcn_sched_group_barrier(0x008, 2 * kProducts - kReads, 0);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");     // the stages are free
     float *mine = reinterpret_cast<float *>(lds) + wave * kAccLen;
@@ -892,6 +895,17 @@ int launch_product(mqg_ctx *ctx, ProductArgs a, int64_t mats, Kernel kernel, hip
         const int grid = tiles_of(64);
         MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product_few<EPI, 1, 2, 2><<<grid, kFewWaves * kWave, 0, s>>>(a)));
         return MQG_OK;
+    }
+    if constexpr (!symmetric) {
+        // Whole rounds of tiles of 256, one to a compute unit: half the operands' traffic.  8,192 x 4,096: 763 -> 698 us (1,180 TFLOP/s of f16 products; the same
+        // without any traffic 572, with the products alone 525: the card's clock falls to 1.5 GHz under them), 4,096^2 390 -> 356; 24 of 1,024^2, a round and a half, 180 and 198.
+        if (a.m % 256 == 0 && a.n % 256 == 0) {
+            const int64_t wide = tiles_of(256), rounds = ceil_div(wide, 256);
+            if (wide * 10 >= rounds * 256 * 9) {
+                MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product<EPI, 2, 4, 4, 2><<<static_cast<int>(wide), 512, 0, s>>>(a)));
+                return MQG_OK;
+            }
+        }
     }
     const int all = tiles_of(128), rest = all > kTileRound && all % kTileRound <= kTileRest ? all % kTileRound : 0;
     MQG_LAUNCH(ctx, names[EPI], s, (k_orth_product<EPI, 2, 2, 2, 2><<<all - rest, 256, 0, s>>>(a)));

@@ -285,9 +285,9 @@ def test_refusals(mqg, ctx):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("mats,rows,cols", [(1, 70, 900), (3, 900, 70), (1, 40, 700), (2, 700, 40), (1, 128, 4000), (1, 4000, 100), (40, 128, 1000), (9, 100, 130), (500, 20, 30),
-                                            (1, 1, 3000), (3, 100, 160), (1, 160, 96), (1, 1030, 1100), (3, 600, 1300), (1, 2200, 2200)])
+                                            (1, 1, 3000), (3, 100, 160), (1, 160, 96), (1, 1030, 1100), (3, 600, 1300), (1, 2200, 2200), (4, 2000, 2040), (1, 4000, 4090)])
 def test_matrices_by_every_kernel(mqg, ctx, mats, rows, cols, dtype):
-    """One launch, few rows or columns, single blocks, tiles of 64 and of 128 and the last tiles of a round."""
+    """One launch, few rows or columns, single blocks, tiles of 64, of 128 and of 256 and the last tiles of a round."""
     gen = torch.Generator(device="cuda")
     gen.manual_seed(mats + rows * 7 + cols)
     u = torch.randn((mats, rows, cols), generator=gen, device="cuda") + torch.randn((mats, rows, 3), generator=gen, device="cuda") @ torch.randn((mats, 3, cols), generator=gen, device="cuda")
