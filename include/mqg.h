@@ -5,6 +5,8 @@
  * that the MQ-GNN paper describes around its pipeline: node-wise neighbour
  * sampling, the mini-batch's topology and feature parts, the GPU feature
  * cache with host fallback, and the gather/aggregate (GA) step of GraphSAGE.
+ * Beside them stand the calls of the layers that read what they produce: norm,
+ * aggregation of 8-bit rows, and the step of the weight matrices.
  *
  * Conventions
  *   - Every pointer named *_dev / documented "device" must be dereferenceable
@@ -643,7 +645,7 @@ int mqg_weighted_aggregate_backward(mqg_ctx *ctx, const mqg_block *block, const 
  * written.  mqg_ctx_reserve_layer allocates now what mqg_rms_norm_backward (for rows of up to norm_dim
  * columns) and mqg_orthogonalize and mqg_muon_step (for stacks of num_mats matrices of rows x cols) would
  * otherwise allocate when they are first called at that size, after a synchronisation of the stream:
- * 4 KiB per column; 12 bytes per element and 8 per element of the smaller side's square, sides rounded up to multiples of 128.
+ * 2 KiB per column; 12 bytes per element and 8 per element of the smaller side's square, sides rounded up to multiples of 128.
  * While a stream is recorded into a HIP graph nothing is allocated: a call that would have to is
  * refused with MQG_ERR_UNSUPPORTED.  Pass 0 for what is not wanted.
  */
@@ -665,7 +667,7 @@ int mqg_ctx_reserve_layer(mqg_ctx *ctx, int32_t norm_dim, int32_t num_mats, int3
  *              q = y / scale rounded to nearest, ties to even.  A group that holds a value that is
  *              not finite has the scale NaN, so that all its values read NaN.
  *              q: device bytes [cap_rows x q_stride], scale: device float [cap_rows x scale_stride]
- * A row of zeros gives zeros.  sum, y and q may each be the buffer of x or residual if the strides in bytes are the same.
+ * A row of zeros gives zeros.  sum and y may each be the buffer of x or of residual if its stride is the same.
  * dim <= MQG_NORM_MAX_DIM.
  */
 #define MQG_NORM_MAX_DIM 16384

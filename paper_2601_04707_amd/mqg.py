@@ -2,7 +2,8 @@
 
 The four operations keep the names of the C ABI (``include/mqg.h``):
 ``mqg_build_cache``, ``mqg_sample_blocks``, ``mqg_gather_features`` and
-``mqg_sage_mean_aggregate``.  Torch is used for device memory, pinned host
+``mqg_sage_mean_aggregate``, and so do the calls of a layer (``mqg_rms_norm``,
+``mqg_muon_step`` and those between them in this file).  Torch is used for device memory, pinned host
 memory and streams; every step of the path runs in the library's kernels.
 There is no fallback: if the shared library is missing, importing this module
 raises.
