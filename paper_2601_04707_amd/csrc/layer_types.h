@@ -19,20 +19,6 @@ struct Vec {
     typedef Whole Any __attribute__((aligned(sizeof(T))));
 };
 
-// Vector number i of a row of dim elements, zeros past its end; nothing outside the row is read.
-template <typename T>
-__device__ __forceinline__ typename Vec<T>::Whole load_raw(const T *row, int i, int dim) {
-    constexpr int V = Vec<T>::kLen;
-    typename Vec<T>::Whole v;
-    if ((i + 1) * V <= dim) {
-        v = *reinterpret_cast<const typename Vec<T>::Any *>(row + i * V);
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = i * V + j < dim ? row[i * V + j] : static_cast<T>(0.f);
-    }
-    return v;
-}
-
 // Vector number i of a row of dim elements as 32-bit numbers, zeros past its end; nothing outside the row is read.
 template <typename T>
 __device__ __forceinline__ void load_vec(const T *row, int i, int dim, float (&out)[Vec<T>::kLen]) {
@@ -47,17 +33,15 @@ __device__ __forceinline__ void load_vec(const T *row, int i, int dim, float (&o
     }
 }
 
-// The same vector of a row that is written: rounded once, to nearest even; nothing outside the row is written.  PAST: not to be kept in the caches
-// (a template's argument: of a branch on it the compiler makes one store of the usual kind)
-template <bool PAST = false, typename T>
+// The same vector of a row that is written: rounded once, to nearest even; nothing outside the row is written.
+template <typename T>
 __device__ __forceinline__ void store_vec(T *row, int i, int dim, const float (&in)[Vec<T>::kLen]) {
     constexpr int V = Vec<T>::kLen;
     if ((i + 1) * V <= dim) {
         typename Vec<T>::Whole v;
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = static_cast<T>(in[j]);
-        if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<typename Vec<T>::Any *>(row + i * V));
-        else *reinterpret_cast<typename Vec<T>::Any *>(row + i * V) = v;
+        *reinterpret_cast<typename Vec<T>::Any *>(row + i * V) = v;
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)
@@ -65,15 +49,61 @@ __device__ __forceinline__ void store_vec(T *row, int i, int dim, const float (&
     }
 }
 
-// Columns i V to i V + V - 1 of a [dim] vector of floats, zeros past its end; null: ones
+// Vector number i of a row of dim elements without a branch on the lane (one element by element makes the wavefront wait for what it loads): the last
+// vector of a row, and any past it, is the row's last V elements, of which the first `skip` are another lane's.
 template <int V>
-__device__ __forceinline__ void load_weight(const float *w, int i, int dim, float (&out)[V]) {
+struct Span {
+    int base, skip;
+    __device__ __forceinline__ Span() = default;
+    __device__ __forceinline__ Span(int i, int dim) {
+        base = i * V < dim - V ? i * V : dim - V > 0 ? dim - V : 0;
+        skip = i * V - base;
+    }
+    __device__ __forceinline__ bool mine(int j) const { return j >= skip; }
+};
+// Its elements as they lie; nothing outside the row is read, zeros past the end of a row of fewer than V.
+template <typename T>
+__device__ __forceinline__ typename Vec<T>::Whole load_span(const T *row, const Span<Vec<T>::kLen> &at, int dim) {
+    constexpr int V = Vec<T>::kLen;
+    typename Vec<T>::Whole v;
+    if (dim >= V) {
+        v = *reinterpret_cast<const typename Vec<T>::Any *>(row + at.base);
+    } else {
 #pragma unroll
-    for (int h = 0; h < V / 4; ++h) {
-        float x[4] = {1.f, 1.f, 1.f, 1.f};
-        if (w) load_vec(w, i * (V / 4) + h, dim, x);
+        for (int j = 0; j < V; ++j) v[j] = j < dim ? row[j] : static_cast<T>(0.f);
+    }
+    return v;
+}
+// The elements that are its own, rounded once, to nearest even.  PAST: not to be kept in the caches (a template's argument: of a branch on it the
+// compiler makes one store of the usual kind)
+template <bool PAST, typename T>
+__device__ __forceinline__ void store_span(T *row, const Span<Vec<T>::kLen> &at, int dim, const float (&in)[Vec<T>::kLen]) {
+    constexpr int V = Vec<T>::kLen;
+    if (at.skip == 0 && dim >= V) {
+        typename Vec<T>::Whole v;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) out[4 * h + j] = x[j];
+        for (int j = 0; j < V; ++j) v[j] = static_cast<T>(in[j]);
+        if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<typename Vec<T>::Any *>(row + at.base));
+        else *reinterpret_cast<typename Vec<T>::Any *>(row + at.base) = v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (at.mine(j) && at.base + j < dim) row[at.base + j] = static_cast<T>(in[j]);
+    }
+}
+// The same columns of a [dim] vector of floats; null: ones
+template <int V>
+__device__ __forceinline__ void load_weight(const float *w, const Span<V> &at, int dim, float (&out)[V]) {
+    if (w && dim >= V) {
+#pragma unroll
+        for (int h = 0; h < V / 4; ++h) {
+            const typename Vec<float>::Whole x = *reinterpret_cast<const typename Vec<float>::Any *>(w + at.base + 4 * h);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) out[4 * h + j] = x[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) out[j] = !w ? 1.f : j < dim ? w[j] : 0.f;
     }
 }
 

@@ -5,9 +5,11 @@
 //   backward   with R = rsqrt(mean(s^2) + eps) and c = R^2 mean(gy w s):  gx = R (gy w - c s) + gs,  gw = sum over rows of gy s R
 //
 // Both are bound by memory: every input is read once and every output written once, a row stays in registers in between.  A row
-// is the work of 4 to 64 lanes of a wavefront, of four wavefronts or of sixteen, by its length: as few as hold it with up to
-// four vectors of 16 bytes each, so that a reduction over the row is a few exchanges between lanes and rows that are
-// short fill the wavefront.
+// is the work of 4 to 64 lanes of a wavefront, of 256, 512 or 1,024 threads, by its length, so that a reduction over a short row is a few exchanges between
+// lanes and short rows fill the wavefront.  Measured, of the 6.2 TB/s that an elementwise kernel reads and writes at: forward 295,000 x 256 fp16 into e4m3
+// 97 us = 5.4, 109,000 x 602 fp32 184 us = 5.7, 20,000 x 2,048 fp32 108 us = 6.1; backward 295,000 x 256 fp16 104 us = 5.8, 8,192 x 8,192 bf16 107 us = 5.0.  The
+// last vector of a row is loaded without a branch (Span): element by element, backward rows of 250 fp16 columns took 227 us instead of 116, of 100 fp32 columns 412
+// instead of 188, for the wait in that branch, which held up the row that was on its way.
 #include <algorithm>
 
 #include "common.h"
@@ -113,7 +115,7 @@ __device__ __forceinline__ Scale scale_of(uint32_t most, float r, float top) {
 
 // V values of a row in 8 bits
 template <int V>
-__device__ __forceinline__ void store_q(uint8_t *row, int i, int dim, const float (&z)[V], const Scale &s, int q_type) {
+__device__ __forceinline__ void store_q(uint8_t *row, const Span<V> &at, int dim, const float (&z)[V], const Scale &s, int q_type) {
     const float inv = 1.0f / s.div;
     float y[V];
 #pragma unroll
@@ -140,7 +142,7 @@ __device__ __forceinline__ void store_q(uint8_t *row, int i, int dim, const floa
             }
         }
     }
-    if ((i + 1) * V <= dim) {
+    if (at.skip == 0 && dim >= V) {
         typedef uint32_t Words __attribute__((ext_vector_type(V / 4)));
         typedef Words AnyWords __attribute__((aligned(1)));
         Words v;
@@ -149,11 +151,11 @@ __device__ __forceinline__ void store_q(uint8_t *row, int i, int dim, const floa
             if constexpr (V == 4) v = w[k];
             else v[k] = w[k];
         }
-        *reinterpret_cast<AnyWords *>(row + i * V) = v;
+        *reinterpret_cast<AnyWords *>(row + at.base) = v;
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            if (i * V + j < dim) row[i * V + j] = static_cast<uint8_t>(w[j / 4] >> (8 * (j % 4)));
+            if (at.mine(j) && at.base + j < dim) row[at.base + j] = static_cast<uint8_t>(w[j / 4] >> (8 * (j % 4)));
     }
 }
 
@@ -170,28 +172,42 @@ k_rms_norm(NormArgs a) {
     const int dim = a.dim;
     const float top = a.q_type == MQG_Q_E4M3 ? 448.f : 127.f;
     const int group_lanes = a.group / V;                   // lanes that share a scale, 0 = the row's
+    const bool full = dim == LANES * NV * V;               // every lane's vectors are its own
     float w[NV][V];
+    Span<V> at[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) load_weight(a.weight, k * LANES + lane, dim, w[k]);
+    for (int k = 0; k < NV; ++k) {
+        at[k] = Span<V>(k * LANES + lane, dim);
+        load_weight(a.weight, at[k], dim, w[k]);
+    }
     for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; row < n; row += int64_t(gridDim.x) * kRows) {
-        float s[NV][V];
+        using W = typename Vec<T>::Whole;
+        W raw[NV], more[NV];
         const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+        const T *r0 = static_cast<const T *>(a.residual) + row * a.residual_stride;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) load_vec(x, k * LANES + lane, dim, s[k]);
-        if (a.residual) {
-            const T *r = static_cast<const T *>(a.residual) + row * a.residual_stride;
-            float t[NV][V];
+        for (int k = 0; k < NV; ++k) {
+            raw[k] = load_span(x, at[k], dim);
+            if (a.residual) more[k] = load_span(r0, at[k], dim);
+        }
+        float s[NV][V];
 #pragma unroll
-            for (int k = 0; k < NV; ++k) load_vec(r, k * LANES + lane, dim, t[k]);
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                s[k][j] = static_cast<float>(raw[k][j]);
+                if (a.residual) s[k][j] += static_cast<float>(more[k][j]);
+            }
+        if (!full) {
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int j = 0; j < V; ++j) s[k][j] += t[k][j];
+                for (int j = 0; j < V; ++j) s[k][j] = at[k].mine(j) ? s[k][j] : 0.f;
         }
         if (a.sum) {
             T *sum = static_cast<T *>(a.sum) + row * a.sum_stride;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) store_vec<PAST>(sum, k * LANES + lane, dim, s[k]);
+            for (int k = 0; k < NV; ++k) store_span<PAST>(sum, at[k], dim, s[k]);
         }
         float squares = 0.f;
 #pragma unroll
@@ -214,7 +230,7 @@ k_rms_norm(NormArgs a) {
                 float v[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) v[j] = s[k][j] * r;
-                store_vec<PAST>(y, k * LANES + lane, dim, v);
+                store_span<PAST>(y, at[k], dim, v);
             }
         }
         if (!a.q) continue;
@@ -234,7 +250,7 @@ k_rms_norm(NormArgs a) {
             const Scale sc = scale_of(lanes.max(m), r, top);
             if (lane == 0) scale[0] = sc.scale;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) store_q(q, k * LANES + lane, dim, s[k], sc, a.q_type);
+            for (int k = 0; k < NV; ++k) store_q(q, at[k], dim, s[k], sc, a.q_type);
         } else {
             const int width = group_lanes < LANES ? group_lanes : LANES;
 #pragma unroll
@@ -242,7 +258,7 @@ k_rms_norm(NormArgs a) {
                 const Scale sc = scale_of(lanes_max(most[k], width), r, top);
                 const int i = k * LANES + lane;
                 if (lane % width == 0 && i * V < dim) scale[i / group_lanes] = sc.scale;
-                store_q(q, i, dim, s[k], sc, a.q_type);
+                store_q(q, at[k], dim, s[k], sc, a.q_type);
             }
         }
     }
@@ -274,10 +290,13 @@ k_rms_norm_backward(NormGradArgs a) {
     const int lane = static_cast<int>(threadIdx.x) % LANES;
     const int64_t n = rows_of(a.num_rows, a.cap_rows);
     const int dim = a.dim;
+    const bool full = dim == LANES * NV * V;               // every lane's vectors are its own
     float w[NV][V], gw[NV][V];
+    Span<V> at[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        load_weight(a.weight, k * LANES + lane, dim, w[k]);
+        at[k] = Span<V>(k * LANES + lane, dim);
+        load_weight(a.weight, at[k], dim, w[k]);
 #pragma unroll
         for (int j = 0; j < V; ++j) gw[k][j] = 0.f;
     }
@@ -291,9 +310,9 @@ k_rms_norm_backward(NormGradArgs a) {
         const T *gs = static_cast<const T *>(a.grad_sum) + row * a.gs_stride;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            v.s[k] = load_raw(sr, k * LANES + lane, dim);
-            v.g[k] = load_raw(gr, k * LANES + lane, dim);
-            if (a.grad_sum) v.gs[k] = load_raw(gs, k * LANES + lane, dim);
+            v.s[k] = load_span(sr, at[k], dim);
+            v.g[k] = load_span(gr, at[k], dim);
+            if (a.grad_sum) v.gs[k] = load_span(gs, at[k], dim);
         }
         return v;
     };
@@ -304,8 +323,17 @@ k_rms_norm_backward(NormGradArgs a) {
     Row next;
     if (kAhead && row < n) next = load(row);
     for (; row < n; row += step) {
-        const Row v = kAhead ? next : load(row);
+        Row v = kAhead ? next : load(row);
         if (kAhead && row + step < n) next = load(row + step);
+        if (!full) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    v.s[k][j] = at[k].mine(j) ? v.s[k][j] : static_cast<T>(0.f);
+                    v.g[k][j] = at[k].mine(j) ? v.g[k][j] : static_cast<T>(0.f);
+                }
+        }
         float squares = 0.f, dot = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -333,7 +361,7 @@ k_rms_norm_backward(NormGradArgs a) {
                 out[j] = r * (g * w[k][j] - c * s);
                 if (a.grad_sum) out[j] += static_cast<float>(v.gs[k][j]);
             }
-            store_vec<PAST>(gx, k * LANES + lane, dim, out);
+            store_span<PAST>(gx, at[k], dim, out);
         }
     }
     if (!a.parts) return;
@@ -343,8 +371,8 @@ k_rms_norm_backward(NormGradArgs a) {
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const int col = (k * LANES + lane) * V + j;
-                if (col < dim) part[col] = gw[k][j];
+                const int col = at[k].base + j;
+                if (at[k].mine(j) && col < dim) part[col] = gw[k][j];
             }
     } else {
         const int wave = static_cast<int>(threadIdx.x) >> 6;
@@ -355,7 +383,7 @@ k_rms_norm_backward(NormGradArgs a) {
                 float v = gw[k][j];
 #pragma unroll
                 for (int off = LANES; off < kWave; off <<= 1) v += __shfl_xor(v, off, kWave);
-                if (lane_id() < LANES) lds[wave * kCols + (k * LANES + lane) * V + j] = v;
+                if (lane_id() < LANES && at[k].mine(j)) lds[wave * kCols + at[k].base + j] = v;
             }
         __syncthreads();
         for (int col = static_cast<int>(threadIdx.x); col < dim; col += kThreads) {
@@ -438,7 +466,7 @@ RowShape row_shape(int dim, int vec, int64_t rows) {
     }
 
 // A call that moves twice what the chip's memory-side cache holds leaves little of its own output there: that goes past the caches (109,000 x 602
-// fp32 rows, four times 262 MB: 213 -> 201 us; 295,000 x 256 fp16 109 -> 102).  Smaller ones keep it for the next reader.
+// fp32 rows, four times 262 MB: 213 -> 203 us; 295,000 x 256 fp16, four times 151 MB: 109 -> 103).  Smaller ones keep it for the next reader.
 constexpr int64_t kPastBytes = int64_t(512) << 20;
 
 template <typename T>
