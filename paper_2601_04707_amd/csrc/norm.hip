@@ -493,9 +493,16 @@ template <typename T>
 int launch_norm_backward(mqg_ctx *ctx, NormGradArgs a, float *grad_weight, hipStream_t s) {
     const RowShape sh = row_shape(a.dim, Vec<T>::kLen, a.cap_rows);
     const int threads = std::max(sh.lanes, kBlock);
-    const int grid = static_cast<int>(std::min<int64_t>(ceil_div(a.cap_rows, threads / sh.lanes), kNormParts));
+    const int64_t sets = ceil_div(a.cap_rows, threads / sh.lanes);
+    // Rows of a few rounds are one workgroup's, whose sum is the gradient, and the second launch falls away: 1 to 64 rows of 64 fp32 9.1 to 9.5 us a call
+    // against 6.7 to 7.2, four of 1,024 bf16 9.2 against 6.6, two of 8,192 9.3 against 8.5.  Further rounds cost more than they save: eight rows of 1,024
+    // 9.1 against 9.0 (waited for: 20.9 against 23.2), four of 8,192 9.3 against 11.7.
+    const bool alone = grad_weight && sets > 0 && sets <= (sh.lanes <= kBlock ? 4 : 2);
+    const int grid = alone ? 1 : static_cast<int>(std::min<int64_t>(sets, kNormParts));
     const bool past = a.cap_rows * a.dim * (a.grad_sum ? 4 : 3) * int64_t(sizeof(T)) >= kPastBytes;
-    if (grad_weight) {
+    if (alone) {
+        a.parts = grad_weight;
+    } else if (grad_weight) {
         int rc = ensure_layer_scratch(ctx, norm_scratch_bytes(a.dim), s, "mqg_rms_norm_backward");
         if (rc != MQG_OK) return rc;
         a.parts = reinterpret_cast<float *>(ctx->layer_scratch);
@@ -509,7 +516,7 @@ int launch_norm_backward(mqg_ctx *ctx, NormGradArgs a, float *grad_weight, hipSt
         MQG_NORM_SHAPES(T, MQG_GO)
     }
 #undef MQG_GO
-    if (grad_weight)
+    if (grad_weight && !alone)
         MQG_LAUNCH(ctx, "k_sum_parts", s,
                    (k_sum_parts<<<static_cast<int>(ceil_div(a.dim, kSumCols)), kSumThreads, 0, s>>>(a.parts, grid, a.dim, grad_weight)));
     return MQG_OK;

@@ -282,6 +282,22 @@ def test_backward_against_differences(mqg, ctx):
         assert abs(got - slope) <= 1e-5 * size
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [5, 64, 250, 1023, 4100, 8200])
+def test_backward_of_a_few_rows(mqg, ctx, dim, dtype):
+    """Rows that one workgroup takes by itself, the first that it does not, and device counts of less."""
+    gen = torch.Generator().manual_seed(11)
+    w = (1 + 0.3 * torch.randn(dim, generator=gen)).cuda()
+    for rows in (1, 2, 3, 4, 5, 16, 17, 64, 65, 256, 257):
+        s, gy, gs = (torch.randn((rows, dim), generator=gen).to(dtype).cuda() for _ in range(3))
+        for count, valid in ((rows, rows), (rows // 2, rows // 2), (rows + 1, rows), (0, 0)):
+            gx, gw = torch.full_like(s, MARK), torch.full((dim + 2,), MARK, device="cuda")
+            mqg.mqg_rms_norm_backward(ctx, gy, s, w, gx, grad_weight=gw[1:-1], grad_sum=gs, eps=EPS, num_rows=torch.tensor([count], device="cuda"))
+            torch.cuda.synchronize()
+            check_backward(gx[:valid], gw[1:-1], backward64(gy[:valid], s[:valid], w, gs[:valid]), dtype, rows)
+            assert bool((gx[valid:] == MARK).all()) and bool((gw[[0, -1]] == MARK).all())
+
+
 # ---------------------------------------------------------------------------------------------- refusals
 
 def test_refusals(mqg, ctx):
