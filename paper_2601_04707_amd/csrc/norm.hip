@@ -97,7 +97,8 @@ struct RowLanes {
 };
 
 // How a group is taken to 8 bits, from z = s w and the row's r, y = z r.  Values and scale have r in common, so q = z / (max|z| / top) has two roundings before
-// its own and r's is none of them; where that quotient would leave 32 bits' range, or the scale is the least one, q = y / scale.
+// its own and r's is none of them (of a million e4m3 values 0.4 to 0.7 are the neighbour of the one that the formula has in 64 bits, of int8 1.5 to 2; of y divided
+// by its scale in 32 bits 0.7 to 0.9 and 2 to 2.2); where that quotient would leave 32 bits' range, or the scale is the least one, q = y / scale.
 // most: the largest |z|'s bit pattern (patterns of absolute values order as the values do, with infinity and NaN above all others): a group that
 // holds a value that is not finite has the scale NaN, so that all its values read NaN.
 struct Scale {
