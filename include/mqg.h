@@ -647,7 +647,9 @@ int mqg_weighted_aggregate_backward(mqg_ctx *ctx, const mqg_block *block, const 
  * otherwise allocate when they are first called at that size, after a synchronisation of the stream:
  * 2 KiB per column; 12 bytes per element and 8 per element of the smaller side's square, sides rounded up to multiples of 128.
  * While a stream is recorded into a HIP graph nothing is allocated: a call that would have to is
- * refused with MQG_ERR_UNSUPPORTED.  Pass 0 for what is not wanted.
+ * refused with MQG_ERR_UNSUPPORTED.  A recorded call goes on using the scratch that it was recorded with:
+ * that stays allocated until mqg_ctx_destroy, also where later calls need more and get a larger one, and the graph may be
+ * replayed until then (as any call on the context, by one stream at a time).  Pass 0 for what is not wanted.
  */
 int mqg_ctx_reserve_layer(mqg_ctx *ctx, int32_t norm_dim, int32_t num_mats, int32_t rows, int32_t cols);
 

@@ -117,24 +117,33 @@ void free_backward_scratch(mqg_ctx *ctx) {
 
 // Room for what a layer's calls leave between their launches.  Growing it waits for the stream first: earlier work may still use the old one.
 int ensure_layer_scratch(mqg_ctx *ctx, int64_t bytes, hipStream_t s, const char *who) {
-    if (bytes <= ctx->layer_scratch_bytes) return MQG_OK;
+    Arena &a = ctx->layer_scratch;
+    const bool enough = bytes <= a.bytes;
+    if (enough && a.recorded) return MQG_OK;
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     hipError_t e = hipStreamIsCapturing(s, &capture);
+    if (enough) {                                          // (not known: the default stream while another one is recorded)
+        if (e != hipSuccess) (void)hipGetLastError();
+        a.recorded = bytes > 0 && (e != hipSuccess || capture != hipStreamCaptureStatusNone);
+        return MQG_OK;
+    }
     if (e != hipSuccess) return fail(ctx, MQG_ERR_HIP, std::string(who) + ": " + hipGetErrorString(e));
     if (capture != hipStreamCaptureStatusNone)
         return fail(ctx, MQG_ERR_UNSUPPORTED, std::string(who) + ": needs more scratch than the context has while the stream is recorded (mqg_ctx_reserve_layer)");
     e = hipStreamSynchronize(s);
     if (e != hipSuccess) return fail(ctx, MQG_ERR_HIP, std::string(who) + ": " + hipGetErrorString(e));
-    (void)hipFree(ctx->layer_scratch);
-    ctx->layer_scratch = nullptr;
-    ctx->layer_scratch_bytes = 0;
-    e = hipMalloc(reinterpret_cast<void **>(&ctx->layer_scratch), static_cast<size_t>(bytes));
-    if (e != hipSuccess) {
-        ctx->layer_scratch = nullptr;
+    const bool grown = a.grow(
+        bytes,
+        [&](int64_t n) {
+            void *p = nullptr;
+            e = hipMalloc(&p, static_cast<size_t>(n));
+            return e == hipSuccess ? static_cast<char *>(p) : nullptr;
+        },
+        [](char *p) { (void)hipFree(p); });
+    if (!grown) {
         (void)hipGetLastError();
         return fail(ctx, MQG_ERR_HIP, std::string(who) + ": scratch allocation failed: " + hipGetErrorString(e));
     }
-    ctx->layer_scratch_bytes = bytes;
     return MQG_OK;
 }
 
@@ -247,7 +256,7 @@ int mqg_ctx_destroy(mqg_ctx *c) {
     (void)hipFree(c->prio_bitmap);
     (void)hipFree(c->prio_count);
     (void)hipFree(c->cache_arena);
-    (void)hipFree(c->layer_scratch);
+    c->layer_scratch.end([](char *p) { (void)hipFree(p); });
     for (auto &r : c->prof_recs) {
         (void)hipEventDestroy(r.start);
         (void)hipEventDestroy(r.stop);

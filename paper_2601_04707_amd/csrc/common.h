@@ -7,6 +7,7 @@
 #include <string>
 #include <vector>
 
+#include "arena.h"
 #include "mqg.h"
 
 namespace mqg {
@@ -115,8 +116,7 @@ struct mqg_ctx {
     char *cache_arena = nullptr;
     int64_t cache_arena_bytes = 0;
     // what the calls of a layer leave between their launches (norm.hip, orthogonal.hip); grows with the calls, or by mqg_ctx_reserve_layer
-    char *layer_scratch = nullptr;
-    int64_t layer_scratch_bytes = 0;
+    mqg::Arena layer_scratch;
     // hash-table dedup (MQG_OPT_DEDUP_HASH); allocated when the option is first used
     bool dedup_hash = false;
     unsigned long long *hash_table = nullptr;      // [hash_capacity] (id << 32 | position), all ones = empty

@@ -506,7 +506,7 @@ int launch_norm_backward(mqg_ctx *ctx, NormGradArgs a, float *grad_weight, hipSt
     } else if (grad_weight) {
         int rc = ensure_layer_scratch(ctx, norm_scratch_bytes(a.dim), s, "mqg_rms_norm_backward");
         if (rc != MQG_OK) return rc;
-        a.parts = reinterpret_cast<float *>(ctx->layer_scratch);
+        a.parts = reinterpret_cast<float *>(ctx->layer_scratch.data);
     }
 #define MQG_GO(T, L, N)                                                                                                        \
     do {                                                                                                                       \

@@ -978,8 +978,8 @@ int run_orthogonalize(mqg_ctx *ctx, const OrthCall &call, hipStream_t s) {
     const OrthLayout l = orth_layout(mats, rows, cols);
     int rc = ensure_layer_scratch(ctx, l.bytes, s, call.who);
     if (rc != MQG_OK) return rc;
-    u.parts = reinterpret_cast<double *>(ctx->layer_scratch);
-    F16 *x = reinterpret_cast<F16 *>(ctx->layer_scratch + l.parts);          // X: n rows of k values
+    u.parts = reinterpret_cast<double *>(ctx->layer_scratch.data);
+    F16 *x = reinterpret_cast<F16 *>(ctx->layer_scratch.data + l.parts);          // X: n rows of k values
     F16 *xt[2] = {x + mats * l.x, x + 2 * mats * l.x};                       // its transpose, in turns
     F16 *gram = x + 3 * mats * l.x, *poly = gram + mats * l.g;
     const bool tall = rows > cols;
