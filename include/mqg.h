@@ -644,7 +644,8 @@ int mqg_weighted_aggregate_backward(mqg_ctx *ctx, const mqg_block *block, const 
  * element only, and, unlike in the calls above, nothing outside a row's dim columns is read or
  * written.  mqg_ctx_reserve_layer allocates now what mqg_rms_norm_backward (for rows of up to norm_dim
  * columns) and mqg_orthogonalize and mqg_muon_step (for stacks of num_mats matrices of rows x cols) would
- * otherwise allocate when they are first called at that size, after a synchronisation of the stream:
+ * otherwise allocate when they are first called at that size, after a synchronisation of their stream
+ * (it synchronises the device itself where it replaces smaller scratch, and is not for a time at which a stream is recorded):
  * 2 KiB per column; 12 bytes per element and 8 per element of the smaller side's square, sides rounded up to multiples of 128.
  * While a stream is recorded into a HIP graph nothing is allocated: a call that would have to is
  * refused with MQG_ERR_UNSUPPORTED.  A recorded call goes on using the scratch that it was recorded with:

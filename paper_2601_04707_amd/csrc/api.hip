@@ -115,7 +115,23 @@ void free_backward_scratch(mqg_ctx *ctx) {
     ctx->bwd_nnz_cap = ctx->bwd_src_cap = 0;
 }
 
-// Room for what a layer's calls leave between their launches.  Growing it waits for the stream first: earlier work may still use the old one.
+// Room for what a layer's calls leave between their launches.
+static int grow_layer_scratch(mqg_ctx *ctx, int64_t bytes, const char *who) {
+    hipError_t e = hipSuccess;
+    const bool grown = ctx->layer_scratch.grow(
+        bytes,
+        [&](int64_t n) {
+            void *p = nullptr;
+            e = hipMalloc(&p, static_cast<size_t>(n));
+            return e == hipSuccess ? static_cast<char *>(p) : nullptr;
+        },
+        [](char *p) { (void)hipFree(p); });
+    if (grown) return MQG_OK;
+    (void)hipGetLastError();
+    return fail(ctx, MQG_ERR_HIP, std::string(who) + ": scratch allocation failed: " + hipGetErrorString(e));
+}
+
+// For a call on s.  Growing it waits for the stream first: earlier work may still use the old one.
 int ensure_layer_scratch(mqg_ctx *ctx, int64_t bytes, hipStream_t s, const char *who) {
     Arena &a = ctx->layer_scratch;
     const bool enough = bytes <= a.bytes;
@@ -132,19 +148,15 @@ int ensure_layer_scratch(mqg_ctx *ctx, int64_t bytes, hipStream_t s, const char 
         return fail(ctx, MQG_ERR_UNSUPPORTED, std::string(who) + ": needs more scratch than the context has while the stream is recorded (mqg_ctx_reserve_layer)");
     e = hipStreamSynchronize(s);
     if (e != hipSuccess) return fail(ctx, MQG_ERR_HIP, std::string(who) + ": " + hipGetErrorString(e));
-    const bool grown = a.grow(
-        bytes,
-        [&](int64_t n) {
-            void *p = nullptr;
-            e = hipMalloc(&p, static_cast<size_t>(n));
-            return e == hipSuccess ? static_cast<char *>(p) : nullptr;
-        },
-        [](char *p) { (void)hipFree(p); });
-    if (!grown) {
-        (void)hipGetLastError();
-        return fail(ctx, MQG_ERR_HIP, std::string(who) + ": scratch allocation failed: " + hipGetErrorString(e));
-    }
-    return MQG_OK;
+    return grow_layer_scratch(ctx, bytes, who);
+}
+
+// Beforehand, for calls on any stream: earlier work may be on any, so growing it waits for the device.
+int reserve_layer_scratch(mqg_ctx *ctx, int64_t bytes, const char *who) {
+    if (bytes <= ctx->layer_scratch.bytes) return MQG_OK;
+    const hipError_t e = ctx->layer_scratch.data ? hipDeviceSynchronize() : hipSuccess;
+    if (e != hipSuccess) return fail(ctx, MQG_ERR_HIP, std::string(who) + ": " + hipGetErrorString(e));
+    return grow_layer_scratch(ctx, bytes, who);
 }
 
 }  // namespace mqg
@@ -780,8 +792,8 @@ int mqg_ctx_reserve_layer(mqg_ctx *ctx, int32_t norm_dim, int32_t num_mats, int3
         if (norm_dim < 0 || num_mats < 0 || rows < 0 || cols < 0) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_ctx_reserve_layer: negative size");
         if (norm_dim > MQG_NORM_MAX_DIM || num_mats > MQG_ORTH_MAX_MATS || rows > MQG_ORTH_MAX_SIDE || cols > MQG_ORTH_MAX_SIDE)
             return fail(ctx, MQG_ERR_UNSUPPORTED, "mqg_ctx_reserve_layer: above the calls' limits");
-        return mqg::ensure_layer_scratch(ctx, std::max(mqg::norm_scratch_bytes(norm_dim), mqg::orth_scratch_bytes(num_mats, rows, cols)), nullptr,
-                                         "mqg_ctx_reserve_layer");
+        return mqg::reserve_layer_scratch(ctx, std::max(mqg::norm_scratch_bytes(norm_dim), mqg::orth_scratch_bytes(num_mats, rows, cols)),
+                                          "mqg_ctx_reserve_layer");
     });
 }
 

@@ -203,6 +203,7 @@ int run_exp_tickets(mqg_ctx *ctx, uint64_t seed, int64_t tag, int64_t first, int
 int run_set_sampling_priority(mqg_ctx *ctx, const mqg_graph *g, const mqg_cache *cache, hipStream_t s);
 // the calls of a layer (norm.hip, aggregate_q8.hip, orthogonal.hip)
 int ensure_layer_scratch(mqg_ctx *ctx, int64_t bytes, hipStream_t s, const char *who);
+int reserve_layer_scratch(mqg_ctx *ctx, int64_t bytes, const char *who);
 int64_t norm_scratch_bytes(int32_t dim);
 int64_t orth_scratch_bytes(int64_t mats, int64_t rows, int64_t cols);
 int run_rms_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const float *weight,

@@ -101,3 +101,24 @@ def test_the_products_refuse_to_allocate_while_recorded(mqg):
                 call()
         assert refused.value.code == mqg.MQG_ERR_UNSUPPORTED and "mqg_ctx_reserve_layer" in str(refused.value)
         torch.cuda.synchronize()
+
+
+def test_reserving_more_waits_for_steps_on_another_stream(mqg):
+    """A step that is still on its way on a stream of its own (which the default stream does not wait for) when its scratch is replaced."""
+    ctx, eager = context(mqg), context(mqg)
+    step, twin = Step(mqg, 3, 1100, 1500), Step(mqg, 3, 1100, 1500)
+    twin(eager)
+    ctx.reserve_layer(norm_dim=96, num_mats=1, rows=1100, cols=1500)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    done = torch.cuda.Event()
+    with torch.cuda.stream(side):
+        for _ in range(3):                                 # (other work before it, so that it is on its way for a while)
+            mqg.mqg_orthogonalize(ctx, step.grad, torch.empty_like(step.grad))
+        step(ctx)
+        done.record()
+    ctx.reserve_layer(num_mats=2, rows=1100, cols=1500)
+    assert done.query()                                    # nothing that had the old scratch is left
+    torch.cuda.synchronize()
+    for got, want in zip(step.outputs(), twin.outputs()):
+        assert torch.equal(got, want)
