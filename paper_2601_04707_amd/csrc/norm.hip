@@ -42,6 +42,12 @@ __device__ __forceinline__ int64_t rows_of(const int64_t *num_rows, int64_t cap)
     return n < cap ? (n > 0 ? n : 0) : cap;
 }
 
+// A row's factor R from its sum of squares; 0 for a row of zeros without an epsilon, so that zeros give zeros.
+__device__ __forceinline__ float row_factor(float squares, int dim, float eps) {
+    const float mean = squares / static_cast<float>(dim) + eps;
+    return mean == 0.f ? 0.f : 1.0f / sqrtf(mean);
+}
+
 // What the lanes of a row find together.  Rows of several wavefronts exchange through LDS: two buffers in turn, so that one barrier
 // per exchange is enough (who writes a buffer again has passed the barrier behind which all have read it).
 template <int LANES>
@@ -219,7 +225,7 @@ k_rms_norm(NormArgs a) {
             squares += part;
         }
         squares = lanes.sum(squares);
-        const float r = 1.0f / sqrtf(squares / static_cast<float>(dim) + a.eps);
+        const float r = row_factor(squares, dim, a.eps);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -349,7 +355,7 @@ k_rms_norm_backward(NormGradArgs a) {
             dot += d;
         }
         lanes.sum_both(&squares, &dot);
-        const float r = 1.0f / sqrtf(squares / static_cast<float>(dim) + a.eps);
+        const float r = row_factor(squares, dim, a.eps);
         const float c = r * r * (dot / static_cast<float>(dim));
         T *gx = static_cast<T *>(a.grad_x) + row * a.gx_stride;
 #pragma unroll
