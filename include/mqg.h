@@ -670,7 +670,8 @@ int mqg_ctx_reserve_layer(mqg_ctx *ctx, int32_t norm_dim, int32_t num_mats, int3
  *              q = y / scale rounded to nearest, ties to even.  A group that holds a value that is
  *              not finite has the scale NaN, so that all its values read NaN.
  *              q: device bytes [cap_rows x q_stride], scale: device float [cap_rows x scale_stride]
- * A row of zeros gives zeros, with eps = 0 too.  sum and y may each be the buffer of x or of residual if its stride is the same.
+ * A row of zeros gives zeros, with eps = 0 too, and so does a row whose 1/sqrt(...) is above fp32's numbers (a root mean square below
+ * 2^-128); rows of any other size have their norm, whatever becomes of their squares in fp32.  sum and y may each be the buffer of x or of residual if its stride is the same.
  * dim <= MQG_NORM_MAX_DIM.
  */
 #define MQG_NORM_MAX_DIM 16384
@@ -683,7 +684,7 @@ int mqg_rms_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *resi
 /*
  * Its backward.  sum: the forward's s (its x where there was no residual); grad_y: the gradient of y (where y was
  * read in 8 bits: of the values that these stand for, the rounding is taken as the identity); grad_sum: the gradient that reaches s
- * by its other uses, NULL if it has none.  With R = 1/sqrt(mean(s^2) + eps), 0 for a row of zeros where eps is 0:
+ * by its other uses, NULL if it has none.  With R = 1/sqrt(mean(s^2) + eps), 0 where the forward gives zeros:
  *   grad_x = R (grad_y * weight - s * R^2 mean(grad_y * weight * s)) + grad_sum   (the gradient of x and of residual)
  *   grad_weight[c] = sum over the rows of grad_y * s * R    (device float [dim], written; NULL if not wanted)
  * Sums in fp32.  grad_weight is made of one sum per workgroup, added in a fixed order: the same bits in every call of the same

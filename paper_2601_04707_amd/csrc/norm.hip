@@ -42,10 +42,23 @@ __device__ __forceinline__ int64_t rows_of(const int64_t *num_rows, int64_t cap)
     return n < cap ? (n > 0 ? n : 0) : cap;
 }
 
-// A row's factor R from its sum of squares; 0 for a row of zeros without an epsilon, so that zeros give zeros.
-__device__ __forceinline__ float row_factor(float squares, int dim, float eps) {
-    const float mean = squares / static_cast<float>(dim) + eps;
-    return mean == 0.f ? 0.f : 1.0f / sqrtf(mean);
+// The mean of squares and eps of a row outside this range: its sums may have lost terms at either end of 32 bits' range, and so may the square of the factor
+// R = 1/sqrt(mean).  They are taken again of s times a power of two, row_unit, after which they are well inside (large: |s| up to 2^128 becomes up to 2^56, sums
+// up to 2^126; small, where eps doesn't make up for the lost terms: 2^-149 to 2^-43 become 2^-59 to 2^47).  Rows of fp16 never need it but for zeros.
+__device__ __forceinline__ bool odd_mean(float mean) {
+    return __float_as_uint(mean) - __float_as_uint(0x1p-100f) > __float_as_uint(0x1p+100f) - __float_as_uint(0x1p-100f);
+}
+__device__ __forceinline__ float row_unit(float mean) { return mean > 0x1p+100f ? 0x1p-72f : mean < 0x1p-100f ? 0x1p+90f : 1.f; }
+// The mean of s times unit, or infinity, whose factor is 0, where the row's own factor, unit times as large, is above 32 bits' numbers: zeros without an epsilon,
+// and rows whose root mean square is below 2^-128.
+__device__ __forceinline__ float unit_mean(float squares, int dim, float eps, float unit) {
+    const float mean = squares / static_cast<float>(dim) + eps * unit * unit;
+    return sqrtf(mean) < unit * 0x1p-128f ? __uint_as_float(0x7F800000u) : mean;
+}
+// What is the same in all lanes of a wavefront, for the compiler, too: scalar registers
+template <int LANES>
+__device__ __forceinline__ float of_wave(float v) {
+    return LANES < kWave ? v : __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
 }
 
 // What the lanes of a row find together.  Rows of several wavefronts exchange through LDS: two buffers in turn, so that one barrier
@@ -224,8 +237,20 @@ k_rms_norm(NormArgs a) {
             for (int j = 0; j < V; ++j) part += s[k][j] * s[k][j];
             squares += part;
         }
-        squares = lanes.sum(squares);
-        const float r = row_factor(squares, dim, a.eps);
+        float mean = of_wave<LANES>(lanes.sum(squares)) / static_cast<float>(dim) + a.eps;
+        if (ballot64(odd_mean(mean))) {                    // (not of rows of several wavefronts: the same in all of them)
+            const float unit = row_unit(mean);
+            squares = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    s[k][j] *= unit;
+                    squares += s[k][j] * s[k][j];
+                }
+            mean = unit_mean(of_wave<LANES>(lanes.sum(squares)), dim, a.eps, unit);
+        }
+        const float r = 1.0f / sqrtf(mean);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -355,8 +380,26 @@ k_rms_norm_backward(NormGradArgs a) {
             dot += d;
         }
         lanes.sum_both(&squares, &dot);
-        const float r = row_factor(squares, dim, a.eps);
-        const float c = r * r * (dot / static_cast<float>(dim));
+        float mean = of_wave<LANES>(squares) / static_cast<float>(dim) + a.eps, unit = 1.f;
+        dot = of_wave<LANES>(dot);
+        if (ballot64(odd_mean(mean))) {
+            unit = row_unit(mean);
+            squares = dot = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float s = static_cast<float>(v.s[k][j]) * unit;
+                    squares += s * s;
+                    dot += static_cast<float>(v.g[k][j]) * w[k][j] * s;
+                }
+            lanes.sum_both(&squares, &dot);
+            mean = unit_mean(of_wave<LANES>(squares), dim, a.eps, unit);
+            dot = of_wave<LANES>(dot);
+        }
+        float r = 1.0f / sqrtf(mean);
+        const float c = r * r * (dot / static_cast<float>(dim)) * unit;
+        r *= unit;
         T *gx = static_cast<T *>(a.grad_x) + row * a.gx_stride;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {

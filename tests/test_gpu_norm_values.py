@@ -72,3 +72,55 @@ def test_rows_of_zeros_without_an_epsilon(mqg, ctx, rows, dim, dtype):
         check_backward(gx, gw, (gx64, terms, gw64, gw_terms), dtype, rows)
         for row in (1, rows - 1):
             assert torch.equal(gx[row], torch.zeros_like(gx[row]) if add is None else add[row])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,dim", [(3, 1), (7, 40), (700, 64), (5, 300), (300, 602), (3, 3000), (300, 8200), (2, 16384)])
+def test_rows_of_any_size(mqg, ctx, rows, dim, dtype):
+    """Rows whose squares leave 32 bits at either end, beside others in between: |s| from 2^-120 to 2^120, and sums near the borders of what is added as it is."""
+    gen = torch.Generator().manual_seed(rows * 3 + dim)
+    size = torch.tensor([-120, -75, -57, -51, -45, 0, 30, 43, 50, 57, 64, 90, 120], dtype=torch.float64)
+    exp = size[torch.arange(rows) % len(size)].unsqueeze(1)
+    for eps in (0.0, 1e-6, 1e-35):
+        s = (torch.randn((rows, dim), generator=gen, dtype=torch.float64) * 2 ** exp).to(dtype).cuda()
+        # gradients of a size at which the results are numbers of 32 bits: grad_x has the size of gy / s
+        gy = (torch.randn((rows, dim), generator=gen, dtype=torch.float64) * 2 ** (exp / 2)).to(dtype).cuda()
+        w = (1 + 0.3 * torch.randn(dim, generator=gen)).cuda()
+        y64, gx64, terms, _, _ = formulas(s, w, gy, None, eps)
+        y, sums = torch.full_like(s, MARK), torch.full_like(s, MARK)
+        q, scale = torch.zeros((rows, dim), dtype=torch.int8, device="cuda"), torch.zeros((rows, 1), device="cuda")
+        mqg.mqg_rms_norm(ctx, s, w, sum_out=sums, y=y, q=q, q_scale=scale, eps=eps)
+        torch.cuda.synchronize()
+        assert torch.equal(sums, s)
+        assert near(y, y64, dtype), eps
+        check_q(q, scale, y64, 0, torch.int8)
+        for start in range(0, min(rows, len(size))):                    # one size at a time: grad_weight's terms are of the size of gy
+            pick = torch.arange(start, rows, len(size)).cuda()
+            part = [t[pick].contiguous() for t in (s, gy)]
+            gx, gw = torch.full_like(part[0], MARK), torch.full((dim,), MARK, device="cuda")
+            mqg.mqg_rms_norm_backward(ctx, part[1], part[0], w, gx, grad_weight=gw, eps=eps)
+            torch.cuda.synchronize()
+            _, gx64, terms, gw64, gw_terms = formulas(part[0], w, part[1], None, eps)
+            check_backward(gx, gw, (gx64, terms, gw64, gw_terms), dtype, rows)
+
+
+@pytest.mark.parametrize("dim", [5, 300, 3000])
+def test_rows_of_the_least_numbers(mqg, ctx, dim):
+    """Rows about the least number of full precision; those whose factor 1/rms is above the largest number of 32 bits count as zeros, in both directions."""
+    gen = torch.Generator().manual_seed(21)
+    noise, gy = torch.randn((6, dim), generator=gen, dtype=torch.float64), (torch.randn((6, dim), generator=gen, dtype=torch.float64) * 2.0 ** -40).float().cuda()
+    for exp in (-124, -140):
+        s = (noise * 2.0 ** exp).float().cuda()
+        y, gx, gw = torch.full_like(s, MARK), torch.full_like(s, MARK), torch.full((dim,), MARK, device="cuda")
+        q, scale = torch.full((6, dim), 3, dtype=torch.int8, device="cuda"), torch.zeros((6, 1), device="cuda")
+        mqg.mqg_rms_norm(ctx, s, None, y=y, q=q, q_scale=scale, eps=0.0)
+        mqg.mqg_rms_norm_backward(ctx, gy, s, None, gx, grad_weight=gw, eps=0.0)
+        torch.cuda.synchronize()
+        if exp == -124:
+            y64, gx64, terms, gw64, gw_terms = formulas(s, None, gy, None, 0.0)
+            assert near(y, y64, torch.float32)
+            check_q(q, scale, y64, 0, torch.int8)
+            check_backward(gx, gw, (gx64, terms, gw64, gw_terms), torch.float32, 6)
+        else:
+            assert bool((y == 0).all()) and bool((q == 0).all()) and bool((scale == 2.0 ** -126).all())
+            assert bool((gx == 0).all()) and bool((gw == 0).all())
