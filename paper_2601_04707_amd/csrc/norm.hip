@@ -221,8 +221,9 @@ k_rms_norm(NormArgs a) {
         if (!full) {
 #pragma unroll
             for (int k = 0; k < NV; ++k)
+                if (at[k].skip > 0)
 #pragma unroll
-                for (int j = 0; j < V; ++j) s[k][j] = at[k].mine(j) ? s[k][j] : 0.f;
+                    for (int j = 0; j < V; ++j) s[k][j] = at[k].mine(j) ? s[k][j] : 0.f;
         }
         if (a.sum) {
             T *sum = static_cast<T *>(a.sum) + row * a.sum_stride;
@@ -268,6 +269,13 @@ k_rms_norm(NormArgs a) {
         if (!a.q) continue;
         uint8_t *q = a.q + row * a.q_stride;
         float *scale = a.scale + row * a.scale_stride;
+        if (!full) {                                       // (another lane's columns: zero times a weight that is not finite would be no number)
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (at[k].skip > 0)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) s[k][j] = at[k].mine(j) ? s[k][j] : 0.f;
+        }
         uint32_t most[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -365,6 +373,13 @@ k_rms_norm_backward(NormGradArgs a) {
                     v.s[k][j] = at[k].mine(j) ? v.s[k][j] : static_cast<T>(0.f);
                     v.g[k][j] = at[k].mine(j) ? v.g[k][j] : static_cast<T>(0.f);
                 }
+        }
+        if (!full) {                                       // (after a row's loads are on their way: before, they would wait for the weight's)
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (at[k].skip > 0)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) w[k][j] = at[k].mine(j) ? w[k][j] : 0.f;
         }
         float squares = 0.f, dot = 0.f;
 #pragma unroll

@@ -124,3 +124,39 @@ def test_rows_of_the_least_numbers(mqg, ctx, dim):
         else:
             assert bool((y == 0).all()) and bool((q == 0).all()) and bool((scale == 2.0 ** -126).all())
             assert bool((gx == 0).all()) and bool((gw == 0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("dim,group,col", [(66, 64, 62), (130, 128, 126), (602, 64, 575), (2050, 32, 2047), (33, 32, 31), (8194, 128, 8191), (3, 32, 1), (64, 32, 5)])
+def test_a_weight_that_is_not_finite_is_its_columns_alone(mqg, ctx, dim, group, col, bad, dtype):
+    rows = 5
+    gen = torch.Generator().manual_seed(dim)
+    x = torch.randn((rows, dim), generator=gen).to(dtype).cuda()
+    x[x == 0] = 1
+    w = (1 + 0.3 * torch.randn(dim, generator=gen)).cuda()
+    w[col] = bad
+    others = torch.arange(dim) != col
+    y64 = formulas(x, w, x, None, 1e-6)[0]
+    for kind in (torch.float8_e4m3fn, torch.int8):
+        y = torch.zeros_like(x)
+        q = torch.zeros((rows, dim), dtype=torch.uint8, device="cuda").view(kind)
+        scale = torch.zeros((rows, -(-dim // group)), device="cuda")
+        mqg.mqg_rms_norm(ctx, x, w, y=y, q=q, q_scale=scale, group=group, eps=1e-6)
+        torch.cuda.synchronize()
+        assert near(y[:, others], y64[:, others], dtype) and not bool(y[:, col].isfinite().any())
+        hit = torch.arange(scale.shape[1]) == col // group
+        assert bool(scale[:, hit].isnan().all()) and bool(scale[:, ~hit].isfinite().all())
+        for g in range(scale.shape[1]):
+            if g != col // group:
+                lo, hi = g * group, min(dim, (g + 1) * group)
+                check_q(q[:, lo:hi], scale[:, g:g + 1], y64[:, lo:hi], 0, kind)
+    # backward: the mean has the weight's infinity once, whatever its neighbour's vector repeats; grad_weight does not depend on the weight
+    gy = torch.randn((rows, dim), generator=gen).to(dtype).cuda()
+    gx, gw = torch.zeros_like(x), torch.zeros(dim, device="cuda")
+    mqg.mqg_rms_norm_backward(ctx, gy, x, w, gx, grad_weight=gw, eps=1e-6)
+    torch.cuda.synchronize()
+    _, gx64, _, gw64, gw_terms = formulas(x, w, gy, None, 1e-6)
+    got = gx.double().cpu()
+    assert torch.equal(got.isnan(), gx64.isnan()) and torch.equal(got.nan_to_num(), gx64.nan_to_num(posinf=float(got.nan_to_num().max()), neginf=float(got.nan_to_num().min())))
+    assert bool(((gw.double().cpu() - gw64).abs() <= (rows + 60) * 2.0 ** -24 * gw_terms + 1e-30).all())
