@@ -114,9 +114,9 @@ k_mean_aggregate_q8(MeanQ8Args a) {
         const float count = e > b ? static_cast<float>(e - b) : 1.f, inv = 1.f / count;
         T *out = static_cast<T *>(a.out) + i * a.out_stride;
 #pragma unroll
-        for (int j = 0; j < kCols; ++j) {                  // the quotient by the reciprocal, and its remainder's
-            const float quot = acc[j] * inv;
-            acc[j] = fmaf(fmaf(-quot, count, acc[j]), inv, quot);
+        for (int j = 0; j < kCols; ++j) {                  // the quotient by the reciprocal, and its remainder's, which infinity has none of
+            const float quot = acc[j] * inv, whole = fmaf(fmaf(-quot, count, acc[j]), inv, quot);
+            acc[j] = fabsf(quot) < __uint_as_float(0x7F800000u) ? whole : quot;
         }
         if (own == at && !narrow) {
             constexpr int V = Vec<T>::kLen;
