@@ -729,7 +729,7 @@ typedef struct mqg_orth {
  * The orthogonal factor of every matrix of a stack, by Newton-Schulz products: X = U / (|U|_F + eps), then per step
  *   A = X X^T,  X <- a X + (b A + c A^2) X          (with X^T X where U has more rows than columns)
  * which takes every singular value x to a x + b x^3 + c x^5 and keeps the singular vectors.  The usual coefficients take singular values
- * from about 0.001 up to 0.7 .. 1.2 in five steps; smaller ones stay smaller.  Rows and columns of zeros stay zeros; a matrix that holds a value that is not finite
+ * from about 0.001 up to 0.7 .. 1.2 in five steps; smaller ones stay smaller.  Rows and columns of zeros stay zeros, matrices of zeros with eps = 0 too; a matrix that holds a value that is not finite
  * gives one without a finite value.
  * Products are exact to about 22 bits with sums in fp32, whatever the types.  Coefficients that take singular values of up to
  * 1 above 256 are refused with MQG_ERR_UNSUPPORTED.

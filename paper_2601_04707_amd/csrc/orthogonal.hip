@@ -98,6 +98,12 @@ k_muon_momentum(UpdateArgs a) {
     if (threadIdx.x == 0) a.parts[int64_t(mat) * gridDim.x + blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
+// unit / (|U| + eps); 0 for a matrix of zeros without an epsilon, so that zeros stay zeros
+__device__ __forceinline__ double unit_over(float unit, double norm, float eps) {
+    const double by = norm + static_cast<double>(eps);
+    return by == 0.0 ? 0.0 : static_cast<double>(unit) / by;
+}
+
 constexpr int kSplitTile = 64;
 
 // X = U / (|U| + eps) times 2^exp in two terms, as U lies (`same`, rows of pad_cols values) and transposed (`turned`, rows of pad_rows values).
@@ -128,8 +134,7 @@ k_orth_split(UpdateArgs a, int num_parts, float unit, F16 *__restrict__ same, F1
     for (int off = 32; off > 0; off >>= 1) squares += __shfl_xor(squares, off, kWave);
     if (lane_id() == 0) lds[threadIdx.x >> 6] = squares;
     __syncthreads();
-    const double norm = sqrt((lds[0] + lds[1]) + (lds[2] + lds[3]));
-    const double inv = static_cast<double>(unit) / (norm + static_cast<double>(a.eps));
+    const double inv = unit_over(unit, sqrt((lds[0] + lds[1]) + (lds[2] + lds[3])), a.eps);
 #pragma unroll
     for (int k = 0; k < kEach; ++k) tile[first + k * kStep][c] = static_cast<float>(update_of(a, v[k], m[k]) * inv);
     __syncthreads();
@@ -666,7 +671,7 @@ k_orth_small(SmallArgs a) {
     for (int k = 0; k < kSmallWaves; ++k) squares += norms[k];
     // unit / (|U| + eps) as a number of 32 bits and a power of two: no product leaves the range of 32 bits on its way
     int exp = 0;
-    const float inv = static_cast<float>(frexp(static_cast<double>(a.unit) / (sqrt(squares) + static_cast<double>(a.u.eps)), &exp));
+    const float inv = static_cast<float>(frexp(unit_over(a.unit, sqrt(squares), a.u.eps), &exp));
     const int chunks = nb * kb * 128;
     constexpr int kChunksEach = kSmallMost * 128 / kThreads;
     auto store_chunk = [&](F16 *to, Half8 hi, Half8 lo) __attribute__((always_inline)) {

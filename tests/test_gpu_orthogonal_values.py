@@ -1,0 +1,45 @@
+"""Matrices of zeros and of the least numbers without an epsilon, orthogonalised and in the weights' step, by every kernel that makes the first iterate."""
+import pytest
+import torch
+
+from test_gpu_orthogonal import USUAL, orth64
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mqg():
+    from paper_2601_04707_amd import mqg as m
+    assert torch.cuda.is_available()
+    return m
+
+
+@pytest.fixture(scope="module")
+def ctx(mqg):
+    g = mqg.Graph(torch.tensor([0, 1, 2], device="cuda"), torch.tensor([1, 0], device="cuda"))
+    return mqg.Context(g, 1, [1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (20, 33), (128, 100), (256, 602), (602, 256)])
+def test_matrices_of_zeros_without_an_epsilon(mqg, ctx, rows, cols, dtype):
+    u = torch.randn((3, rows, cols), generator=torch.Generator().manual_seed(rows)).to(dtype).cuda()
+    u[1] = 0
+    out = torch.full_like(u, 7.0)
+    mqg.mqg_orthogonalize(ctx, u, out, eps=0.0)
+    torch.cuda.synchronize()
+    assert bool((out[1] == 0).all())
+    for i in (0, 2):
+        want, off = orth64(u[i].cpu(), [USUAL] * 5, 0.0)
+        unit = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}[dtype]
+        assert float((out[i].double().cpu() - want).norm()) <= off + unit * float(want.norm()) + 2.0 ** -25 * want.numel() ** 0.5
+
+
+@pytest.mark.parametrize("rows,cols", [(20, 33), (256, 602), (602, 256)])
+def test_a_step_without_a_gradient_keeps_the_weights(mqg, ctx, rows, cols):
+    gen = torch.Generator().manual_seed(3)
+    w = torch.randn((rows, cols), generator=gen).cuda()
+    grad, momentum, before = torch.zeros_like(w), torch.zeros_like(w), w.clone()
+    mqg.mqg_muon_step(ctx, grad, momentum, w, lr=0.02, eps=0.0)
+    torch.cuda.synchronize()
+    assert torch.equal(w, before) and bool((momentum == 0).all())
