@@ -681,8 +681,11 @@ k_orth_small(SmallArgs a) {
     auto chunk_of = [&](const float *from, int step, Half8 *hi, Half8 *lo) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
+            // in this order: a product of numbers below 2^-126 would lose bits; rounded to 32 bits before it is split: the compiler would make one operation of both
+            float v = ldexpf(from[j * step], exp) * inv;
+            asm("" : "+v"(v));
             F16 h, l;
-            split(ldexpf(from[j * step] * inv, exp), &h, &l);
+            split(v, &h, &l);
             (*hi)[j] = h;
             (*lo)[j] = l;
         }

@@ -43,3 +43,15 @@ def test_a_step_without_a_gradient_keeps_the_weights(mqg, ctx, rows, cols):
     mqg.mqg_muon_step(ctx, grad, momentum, w, lr=0.02, eps=0.0)
     torch.cuda.synchronize()
     assert torch.equal(w, before) and bool((momentum == 0).all())
+
+
+@pytest.mark.parametrize("rows,cols", [(20, 33), (33, 20), (64, 64), (256, 602)])
+@pytest.mark.parametrize("exp", [-130, -140])
+def test_matrices_of_the_least_numbers(mqg, ctx, rows, cols, exp):
+    """Below the least number of full precision: they are multiples of 2^-149, exact inputs, and have the orthogonal factor of the same matrix at any other size."""
+    u = (torch.randn((rows, cols), generator=torch.Generator().manual_seed(cols), dtype=torch.float64) * 2.0 ** exp).float()
+    out = torch.zeros((rows, cols), device="cuda")
+    mqg.mqg_orthogonalize(ctx, u.cuda(), out, eps=0.0)
+    torch.cuda.synchronize()
+    want, off = orth64(u, [USUAL] * 5, 0.0)
+    assert float((out.double().cpu() - want).norm()) <= off + 2.0 ** -24 * float(want.norm())
