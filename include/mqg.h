@@ -646,7 +646,9 @@ int mqg_weighted_aggregate_backward(mqg_ctx *ctx, const mqg_block *block, const 
  * columns) and mqg_orthogonalize and mqg_muon_step (for stacks of num_mats matrices of rows x cols) would
  * otherwise allocate when they are first called at that size, after a synchronisation of their stream
  * (it synchronises the device itself where it replaces smaller scratch, and is not for a time at which a stream is recorded):
- * 2 KiB per column; 12 bytes per element and 8 per element of the smaller side's square, sides rounded up to multiples of 128.
+ * 2 KiB per column; 8 KiB per matrix, 12 bytes per element and 8 per element of the smaller side's square, sides rounded up to
+ * multiples of 64 or 128, but nothing for matrices that one workgroup holds (with n and k sides in units of 32, n <= k, rounded up: n k <= 16
+ * and 2 n k + n^2 <= 39, up to 32 x 512, 64 x 256 and 96 x 160).
  * While a stream is recorded into a HIP graph nothing is allocated: a call that would have to is
  * refused with MQG_ERR_UNSUPPORTED.  A recorded call goes on using the scratch that it was recorded with:
  * that stays allocated until mqg_ctx_destroy, also where later calls need more and get a larger one, and the graph may be

@@ -927,7 +927,10 @@ int launch_product(mqg_ctx *ctx, ProductArgs a, int64_t mats, Kernel kernel, hip
 
 }  // namespace
 
-int64_t orth_scratch_bytes(int64_t mats, int64_t rows, int64_t cols) { return mats > 0 && rows > 0 && cols > 0 ? orth_layout(mats, rows, cols).bytes : 0; }
+int64_t orth_scratch_bytes(int64_t mats, int64_t rows, int64_t cols) {
+    if (mats <= 0 || rows <= 0 || cols <= 0 || orth_fits_small(std::min(rows, cols), std::max(rows, cols))) return 0;
+    return orth_layout(mats, rows, cols).bytes;
+}
 
 // Whether the polynomials' values stay in what the iterates are stored in
 bool orth_coeffs_fit(const float *coeffs, int32_t steps) {

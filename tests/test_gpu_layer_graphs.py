@@ -122,3 +122,47 @@ def test_reserving_more_waits_for_steps_on_another_stream(mqg):
     torch.cuda.synchronize()
     for got, want in zip(step.outputs(), twin.outputs()):
         assert torch.equal(got, want)
+
+
+def test_matrices_of_one_workgroup_need_no_scratch(mqg):
+    """Nothing is set aside for them, and nothing has to be: their steps are recorded on a context without scratch."""
+    ctx = context(mqg)
+    torch.cuda.synchronize()
+    for rows, cols in ((32, 512), (512, 32), (64, 256), (96, 160), (160, 96), (1, 1)):
+        before = torch.cuda.mem_get_info()[0]
+        ctx.reserve_layer(num_mats=65_535, rows=rows, cols=cols)
+        assert before - torch.cuda.mem_get_info()[0] < (8 << 20)
+        gen = torch.Generator().manual_seed(rows)
+        grad, weight = (torch.randn((2, rows, cols), generator=gen).cuda() for _ in range(2))
+        momentum, eager = torch.zeros_like(weight), (torch.zeros_like(weight), weight.clone())
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            mqg.mqg_muon_step(ctx, grad, momentum, weight, lr=0.1)
+        for k in range(3):
+            graph.replay()
+            mqg.mqg_muon_step(ctx, grad, *eager, lr=0.1)
+            torch.cuda.synchronize()
+            assert torch.equal(weight, eager[1]) and torch.equal(momentum, eager[0]), k
+    # the next larger ones do
+    for rows, cols in ((33, 512), (64, 257), (96, 161), (97, 97)):
+        other = context(mqg)
+        grad = torch.randn((rows, cols), device="cuda")
+        out = torch.empty_like(grad)
+        torch.cuda.synchronize()
+        with pytest.raises(mqg.MqgError):
+            with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=torch.cuda.Stream()):
+                mqg.mqg_orthogonalize(other, grad, out)
+        torch.cuda.synchronize()
+        other.reserve_layer(num_mats=1, rows=rows, cols=cols)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            mqg.mqg_orthogonalize(other, grad, out)
+        want = torch.empty_like(grad)
+        mqg.mqg_orthogonalize(ctx, grad, want)
+        for _ in range(2):
+            out.fill_(7)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+        del graph
