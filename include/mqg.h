@@ -702,7 +702,7 @@ int mqg_rms_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, c
  *   (group = 0: one scale per row); a destination with no sampled neighbour gets zeros.
  * q: device bytes [num_src x q_stride]; scale: device float [num_src x scale_stride]; out: device [cap_dst x out_stride] of dtype.
  * Sums in fp32 (one that leaves its range is infinite), in an order that depends on the row's entries, dim and dtype alone; one rounding at the store.  Its backward, for the values that q
- * stands for, is mqg_sage_mean_aggregate_backward.
+ * stands for, is mqg_sage_mean_aggregate_backward (of MQG_F32 and MQG_F16 gradients).
  */
 int mqg_sage_mean_aggregate_q8(mqg_ctx *ctx, const mqg_block *block, const void *q, int64_t q_stride, int32_t q_type, int32_t group,
                                const float *scale, int64_t scale_stride, void *out, int64_t out_stride, int32_t dim, int32_t dtype,

@@ -1,8 +1,8 @@
 // GraphSAGE mean aggregation over one block (paper Eq. 16) whose source rows are held in 8 bits with scales:
 //   out[i, c] = (1/n_i) sum over the edges e of row i of scale[indices[e], c / group] q[indices[e], c]
-// What bounds it is the number of random lines of 128 bytes that its input rows and their scales lie in, 57 to 58 G a second whatever the width (the
-// card's rate of random lookups out of tables of this size is 51 to 53): 295,000 rows of 15 entries of 256 columns, three lines to an entry, 215 us; 2.8 M entries of
-// 128 columns 97 us.  8 bits are half of fp16's lines.  Long rows come to 5 to 6.8 TB/s of row bytes.
+// What bounds it is memory: the lines of 128 bytes that its input rows lie in, as often as an entry meets them, and the lookups of their scales.  4.4 M entries
+// of 256 columns out of 1.35 M rows take 239 us, 184 of them (6.2 TB/s of row lines, what an elementwise kernel reaches) without the scales' loads; 2.8 M entries of 128 columns
+// 85, 70 without.  8 bits are half of fp16's lines: the same entries of fp16 rows take k_mean_aggregate 359 and 115 us.
 //
 // 16 columns, 16 bytes, are a lane's; an output row is the work of the smallest power of two of lanes that covers it, up to a wavefront (wider rows:
 // slabs of 1,024 columns, a share of the grid each), so that no sum crosses lanes: the order depends on the row's own entries alone, and the result is

@@ -7,7 +7,7 @@
 // Both are bound by memory: every input is read once and every output written once, a row stays in registers in between.  A row
 // is the work of 4 to 64 lanes of a wavefront, of 256, 512 or 1,024 threads, by its length, so that a reduction over a short row is a few exchanges between
 // lanes and short rows fill the wavefront.  Measured, of the 6.2 TB/s that an elementwise kernel reads and writes at: forward 295,000 x 256 fp16 into e4m3
-// 97 us = 5.4, 109,000 x 602 fp32 184 us = 5.7, 20,000 x 2,048 fp32 108 us = 6.1; backward 295,000 x 256 fp16 104 us = 5.8, 8,192 x 8,192 bf16 107 us = 5.0.  The
+// 97 us = 5.4, 109,000 x 602 fp32 184 to 187 us = 5.6 to 5.7, 20,000 x 2,048 fp32 107 to 109 us = 6.0 to 6.1; backward 295,000 x 256 fp16 104 us = 5.8, 8,192 x 8,192 bf16 107 us = 5.0.  The
 // last vector of a row is loaded without a branch (Span): element by element, backward rows of 250 fp16 columns took 227 us instead of 116, of 100 fp32 columns 412
 // instead of 188, for the wait in that branch, which held up the row that was on its way.
 #include <algorithm>
@@ -45,6 +45,7 @@ __device__ __forceinline__ int64_t rows_of(const int64_t *num_rows, int64_t cap)
 // The mean of squares and eps of a row outside this range: its sums may have lost terms at either end of 32 bits' range, and so may the square of the factor
 // R = 1/sqrt(mean).  They are taken again of s times a power of two, row_unit, after which they are well inside (large: |s| up to 2^128 becomes up to 2^56, sums
 // up to 2^126; small, where eps doesn't make up for the lost terms: 2^-149 to 2^-43 become 2^-59 to 2^47).  Rows of fp16 never need it but for zeros.
+// The comparison costs the others nothing to 1.5 % (300,000 x 100 fp32 66.9 -> 67.8 us).
 __device__ __forceinline__ bool odd_mean(float mean) {
     return __float_as_uint(mean) - __float_as_uint(0x1p-100f) > __float_as_uint(0x1p+100f) - __float_as_uint(0x1p-100f);
 }
@@ -531,7 +532,8 @@ RowShape row_shape(int dim, int vec, int64_t rows) {
     }
 
 // A call that moves twice what the chip's memory-side cache holds leaves little of its own output there: that goes past the caches (109,000 x 602
-// fp32 rows, four times 262 MB: 213 -> 203 us; 295,000 x 256 fp16, four times 151 MB: 109 -> 103).  Smaller ones keep it for the next reader.
+// fp32 rows, four times 262 MB: 202 -> 190 us; 295,000 x 256 bf16, four times 151 MB: 112 -> 97; backward of these 194 -> 191 and 111 -> 108).  Smaller ones
+// keep it for the next reader, though they would be faster by themselves, too (40,000 x 1,000 bf16, 320 MB: 55 -> 49; 60,000 x 256 fp32 42 -> 37).
 constexpr int64_t kPastBytes = int64_t(512) << 20;
 
 template <typename T>
@@ -540,8 +542,10 @@ int launch_norm(mqg_ctx *ctx, const NormArgs &a, hipStream_t s) {
     const int64_t cells = a.cap_rows * a.dim, arrays = 1 + (a.residual != nullptr) + (a.sum != nullptr) + (a.y != nullptr);
     const bool past = cells * (arrays * int64_t(sizeof(T)) + (a.q != nullptr)) >= kPastBytes;
     const int threads = std::max(sh.lanes, kBlock);
-    // A workgroup takes one set of rows (loops of a few workgroups per compute unit read at 4.2 to 5.2 TB/s, this at 4.9 to 5.9), of 16-bit rows, whose weight is
-    // twice as long as they are, several (295,000 x 256 fp16: 118 us with one, 109 with 4.5, 131 with 18).
+    // A workgroup takes one set of rows, of 16-bit rows, whose weight is twice as long as they are, several: 8,192 workgroups of 256 threads at most.
+    // With at most 2,048, 8,192, 16,384 and no limit, us:  fp16 295,000 x 256 into e4m3 106, 101, 98, 100; 300,000 x 100 62, 57, 55, 55; 100,000 x 602 into rows and e4m3
+    // 121, 110, 112, 121; bf16 1 M x 64 52, 42, 45, 55; 40,000 x 1,000 57, 55, 55, 56; 8,192^2 105, 105, 107, 108;  fp32 109,000 x 602 209, 193, 188, 189;
+    // 20,000 x 2,048 120, 110, 105, 107; 295,000 x 256 into e4m3 221, 171, 170, 180; 300,000 x 100 113, 89, 90, 93 and without a residual 59, 48, 50, 65.
     const int64_t most = sizeof(T) == 4 ? (int64_t(1) << 31) - 1 : int64_t(8192) * kBlock / threads;
     const int64_t grid = std::min<int64_t>(std::min<int64_t>(ceil_div(a.cap_rows, threads / sh.lanes), most), ((int64_t(1) << 32) - 1) / threads);
 #define MQG_GO(T, L, N)                                                                                                        \

@@ -589,7 +589,8 @@ __device__ __forceinline__ void quad_transpose(uint32_t (&w)[4]) {
 }
 
 // A matrix whose X, X^T and G (then B) fit a compute unit's LDS, all of it in one launch: a workgroup holds it from the update to the
-// weights.  What bounds it is latency: three products of a few blocks per step, with the LDS written between two barriers.
+// weights.  What bounds it is latency: three products of a few blocks per step, with the LDS written between two barriers: 16 x 16 15.5 us, 64 x 64 20.5, 64 x 256 39.3 for
+// five steps (by the kernels below 57, 70 and 70).
 constexpr int kSmallWaves = 8, kSmallBlocks = 39, kSmallMost = 16;      // blocks of LDS; of X
 inline bool orth_fits_small(int64_t n, int64_t k) {
     const int64_t nb = ceil_div(n, kSide), kb = ceil_div(k, kSide);
