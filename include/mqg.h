@@ -659,7 +659,7 @@ int mqg_ctx_reserve_layer(mqg_ctx *ctx, int32_t norm_dim, int32_t num_mats, int3
 /*
  * Root-mean-square norm of rows, with the residual's addition:
  *   s = x + residual,  y = s * 1/sqrt(mean over the columns of s^2 + eps) * weight
- * computed in fp32 from the inputs; each output is rounded once.
+ * computed in fp32 from the inputs (s * weight first, which has to stay within fp32's range); each output is rounded once.
  *   residual   may be NULL: s = x
  *   weight     device float [dim]; NULL = ones
  *   num_rows_dev  device int64, the number of rows (e.g. &blocks[l].sizes[1]); values above cap_rows
