@@ -5,8 +5,8 @@
  * that the MQ-GNN paper describes around its pipeline: node-wise neighbour
  * sampling, the mini-batch's topology and feature parts, the GPU feature
  * cache with host fallback, and the gather/aggregate (GA) step of GraphSAGE.
- * Beside them stand the calls of the layers that read what they produce: norm,
- * aggregation of 8-bit rows, and the step of the weight matrices.
+ * Beside them stand the calls of the layers that read what they produce: norms,
+ * aggregation of 8-bit rows, and the steps of the weights.
  *
  * Conventions
  *   - Every pointer named *_dev / documented "device" must be dereferenceable
@@ -642,11 +642,11 @@ int mqg_weighted_aggregate_backward(mqg_ctx *ctx, const mqg_block *block, const 
  * context for errors, profiling and scratch only; its graph is not used.  Rows and matrices may
  * be MQG_F32, MQG_F16 or MQG_BF16; strides are in elements, pointers need the alignment of an
  * element only, and, unlike in the calls above, nothing outside a row's dim columns is read or
- * written.  mqg_ctx_reserve_layer allocates now what mqg_rms_norm_backward (for rows of up to norm_dim
+ * written.  mqg_ctx_reserve_layer allocates now what mqg_rms_norm_backward and mqg_layer_norm_backward (for rows of up to norm_dim
  * columns) and mqg_orthogonalize and mqg_muon_step (for stacks of num_mats matrices of rows x cols) would
  * otherwise allocate when they are first called at that size, after a synchronisation of their stream
  * (it synchronises the device itself where it replaces smaller scratch, and is not for a time at which a stream is recorded):
- * 2 KiB per column; 8 KiB per matrix, 12 bytes per element and 8 per element of the smaller side's square, sides rounded up to
+ * 4 KiB per column (the root-mean-square norm takes 2); 8 KiB per matrix, 12 bytes per element and 8 per element of the smaller side's square, sides rounded up to
  * multiples of 64 or 128, but nothing for matrices that one workgroup holds (with n and k sides in units of 32, n <= k, rounded up: n k <= 16
  * and 2 n k + n^2 <= 39, up to 32 x 512, 64 x 256 and 96 x 160).
  * While a stream is recorded into a HIP graph nothing is allocated: a call that would have to is
@@ -695,6 +695,30 @@ int mqg_rms_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *resi
 int mqg_rms_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, const void *sum, int64_t sum_stride, const float *weight,
                           const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows_dev, int64_t cap_rows, int32_t dim,
                           int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, mqg_stream stream);
+
+/*
+ * Layer norm of rows, with the residual's addition:
+ *   s = x + residual,  d = s - mean over the columns of s,  y = d * 1/sqrt(mean over the columns of d^2 + eps) * weight + bias
+ * computed in fp32 from the inputs; each output is rounded once.  Arguments as mqg_rms_norm's, and
+ *   bias   device float [dim]; NULL = zeros
+ * A row of equal values gives the bias, with eps = 0 too, and so does a row whose 1/sqrt(...) is above fp32's numbers (one that spreads less than
+ * 2^-128); rows of any other size and mean have their norm, whatever becomes of their sums and squares in fp32.  A row that holds a value that is not finite gives none that is.
+ */
+int mqg_layer_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const float *weight,
+                   const float *bias, float eps, const int64_t *num_rows_dev, int64_t cap_rows, int32_t dim, int32_t dtype, void *sum,
+                   int64_t sum_stride, void *y, int64_t y_stride, void *q, int64_t q_stride, int32_t q_type, int32_t group, float *scale,
+                   int64_t scale_stride, mqg_stream stream);
+
+/*
+ * Its backward.  With d and R = 1/sqrt(mean(d^2) + eps) of the forward's s, 0 where the forward gives the bias, u = d R and h = grad_y * weight:
+ *   grad_x = R (h - mean(h) - u mean(h u)) + grad_sum   (the gradient of x and of residual)
+ *   grad_weight[c] = sum over the rows of grad_y * u,  grad_bias[c] = sum over the rows of grad_y    (device float [dim], written;
+ *                    NULL if not wanted)
+ * Arguments, sums, their order and buffers in place as mqg_rms_norm_backward's.
+ */
+int mqg_layer_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, const void *sum, int64_t sum_stride, const float *weight,
+                            const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows_dev, int64_t cap_rows, int32_t dim,
+                            int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, float *grad_bias, mqg_stream stream);
 
 /*
  * mqg_sage_mean_aggregate of source rows in 8 bits with scales, as mqg_rms_norm writes them:
@@ -748,6 +772,61 @@ int mqg_orthogonalize(mqg_ctx *ctx, const mqg_matrices *update, const mqg_matric
  */
 int mqg_muon_step(mqg_ctx *ctx, const mqg_matrices *grad, const mqg_matrices *momentum, const mqg_matrices *weight, float lr, float beta,
                   int32_t nesterov, float weight_decay, float scale, const mqg_orth *plan, mqg_stream stream);
+
+/* How the moments of a parameter are held (mqg_adamw_step). */
+typedef enum { MQG_STATE_F32 = 0, MQG_STATE_E4M3 = 1 } mqg_state_type;
+#define MQG_ADAMW_BLOCK 128
+
+/*
+ * A tensor that an optimiser steps: numel elements, one after the other.  What is written (weight, copy, m, v and their scales) overlaps
+ * no other buffer of the call.  Any alignment of the element.
+ */
+typedef struct mqg_param {
+    int64_t numel;
+    void *weight;                        /* device [numel] of weight_type, read and written             */
+    const void *grad;                    /* device [numel] of grad_type; NULL: the tensor is left alone */
+    void *copy;                          /* device [numel] of copy_type, receives the weight rounded to it; NULL if not wanted */
+    void *m, *v;                         /* device [numel]: the moments, float; or bytes with MQG_STATE_E4M3 */
+    float *m_scale, *v_scale;            /* device [ceil(numel / MQG_ADAMW_BLOCK)]: MQG_STATE_E4M3 only */
+    int32_t weight_type, grad_type, copy_type;   /* mqg_dtype                                           */
+    int32_t state_type;                  /* mqg_state_type                                              */
+    float lr_scale, decay_scale;         /* times the plan's lr and weight_decay: 1 in most, decay_scale 0 for biases and the like */
+} mqg_param;
+
+typedef struct mqg_adamw {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;                        /* the number of this step, 1, 2, ...                          */
+    const int64_t *step_dev;             /* device; the same, read when the step runs (below 1: 1); NULL: step */
+    const float *lr_dev;                 /* device; NULL: lr                                            */
+    const float *grad_scale_dev;         /* device; what the gradients are multiplied by; NULL: 1       */
+} mqg_adamw;
+
+/*
+ * The norm of all gradients of a list (their number, grad and grad_type are read; a grad of NULL counts as zeros), and the factor that clips them:
+ *   n = mul * sqrt(sum over all gradients of g^2),   scale = mul * min(1, max_norm / n)
+ * mul: what the gradients are to be multiplied by in any case (1, or one over a loss scale); max_norm: INFINITY = no limit.
+ * norm, scale: device float, either may be NULL.  A norm that is not finite in fp32 gives the scale NaN, with which mqg_adamw_step steps nothing.
+ * Squares are added in fp32 sixteen at a time and in double above, whatever the gradients' size, in an order that depends on the list's sizes and
+ * types alone: the same bits in every call.  Nothing is allocated.
+ */
+int mqg_grad_norm(mqg_ctx *ctx, const mqg_param *params, int32_t num_params, float mul, float max_norm, float *norm, float *scale,
+                  mqg_stream stream);
+
+/*
+ * An AdamW step of every tensor of a list, with g = grad_scale * grad:
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2
+ *   weight <- (1 - lr weight_decay) weight - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32 (no change where the divisor is zero), each result rounded once, to nearest even.  Weights of 16 bits are rounded at every step, which loses steps of
+ * less than half their last place: keep those in MQG_F32 and take a copy of 16 bits.
+ *   MQG_STATE_E4M3   m = m_scale * value and sqrt(v) = v_scale * value, e4m3 values with a scale per MQG_ADAMW_BLOCK elements in order (the last block may be
+ *              shorter), scale = max(max |.| / 448, 2^-126), values rounded to nearest, ties to even, a root above zero to 2^-9 at least.  The step itself
+ *              has the moments before they are rounded.  Zeros (bytes and scales) are the moments before the first step.  Rounding to nearest
+ *              means that a root follows its block's largest one exactly and changes against it once it is half a step (up to a 16th) away.
+ *              A block with a moment that is not finite gets the scale NaN.
+ * A grad_scale that is not finite leaves everything as it is.  A recorded call reads step_dev, lr_dev and grad_scale_dev at every replay; `step` and
+ * `lr` are those it was recorded with.  The list is read during the call only; nothing is allocated.
+ */
+int mqg_adamw_step(mqg_ctx *ctx, const mqg_param *params, int32_t num_params, const mqg_adamw *plan, mqg_stream stream);
 
 /*
  * Depth of the mini-batch queue, i.e. how many mini-batches to keep in flight

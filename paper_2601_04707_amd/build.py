@@ -19,7 +19,7 @@ OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmqg.so")
 
 SOURCES = ["api.hip", "sample.hip", "gather.hip", "aggregate.hip", "edge_order.hip", "cache.hip", "radix.hip", "dedup_hash.hip", "layerwise.hip",
-           "norm.hip", "aggregate_q8.hip", "orthogonal.hip"]
+           "norm.hip", "layer_norm.hip", "aggregate_q8.hip", "orthogonal.hip", "adamw.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

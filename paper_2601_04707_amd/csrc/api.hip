@@ -4,6 +4,8 @@
 #include <cstdint>
 #include <cstring>
 #include <new>
+#include <utility>
+#include <vector>
 
 #include "common.h"
 
@@ -22,6 +24,23 @@ int guarded(F call) {
     } catch (...) {
         return MQG_ERR_HIP;
     }
+}
+
+// The written ranges of one kind of buffer in a list of parameters: two that overlap would be stepped by two workgroups at once.
+template <typename Of>
+bool overlapping(const mqg_param *params, int32_t num, Of of) {
+    std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
+    ranges.reserve(static_cast<size_t>(num));
+    for (int32_t i = 0; i < num; ++i)
+        if (params[i].grad && params[i].numel > 0) {
+            const std::pair<const void *, int64_t> r = of(params[i]);
+            const uintptr_t at = reinterpret_cast<uintptr_t>(r.first);
+            if (r.first) ranges.emplace_back(at, at + static_cast<uintptr_t>(r.second));
+        }
+    if (!std::is_sorted(ranges.begin(), ranges.end())) std::sort(ranges.begin(), ranges.end());
+    for (size_t i = 1; i < ranges.size(); ++i)
+        if (ranges[i].first < ranges[i - 1].second) return true;
+    return false;
 }
 
 template <typename T>
@@ -234,6 +253,7 @@ int mqg_ctx_create(mqg_ctx **out, const mqg_graph *g, int32_t max_seeds, const i
     ok = ok && dev_alloc(&c->hit_list, c->max_src) == hipSuccess;
     ok = ok && dev_alloc(&c->miss_list, c->max_src) == hipSuccess;
     ok = ok && dev_alloc(&c->counters, 8) == hipSuccess;
+    ok = ok && dev_alloc(&c->norm_parts, mqg::kGradNormParts) == hipSuccess;
     if (ok) ok = hipMemset(c->local_of, 0xFF, std::max<int64_t>(c->num_nodes, 1) * sizeof(int32_t)) == hipSuccess;
     if (ok) ok = hipMemset(c->bitmap, 0, bitmaps * c->bitmap_words * sizeof(uint32_t)) == hipSuccess;
     if (ok) ok = hipMemset(c->counters, 0, 8 * sizeof(unsigned long long)) == hipSuccess;
@@ -262,6 +282,7 @@ int mqg_ctx_destroy(mqg_ctx *c) {
     (void)hipFree(c->hit_list);
     (void)hipFree(c->miss_list);
     (void)hipFree(c->counters);
+    (void)hipFree(c->norm_parts);
     mqg::free_backward_scratch(c);
     mqg::free_hash_scratch(c);
     mqg::free_layerwise_scratch(c);
@@ -682,6 +703,42 @@ int mqg_rms_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, c
     });
 }
 
+int mqg_layer_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const float *weight,
+                   const float *bias, float eps, const int64_t *num_rows_dev, int64_t cap_rows, int32_t dim, int32_t dtype, void *sum,
+                   int64_t sum_stride, void *y, int64_t y_stride, void *q, int64_t q_stride, int32_t q_type, int32_t group, float *scale,
+                   int64_t scale_stride, mqg_stream stream) {
+    if (!ctx) return MQG_ERR_INVALID_ARG;
+    return guarded([&]() -> int {
+        int rc = check_norm_rows(ctx, "mqg_layer_norm", cap_rows, dim, dtype, eps);
+        if (rc != MQG_OK) return rc;
+        if (cap_rows > 0 && !y && !q) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_layer_norm: neither y nor q is given");
+        if (cap_rows > 0 && !x) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_layer_norm: x is NULL");
+        if (x_stride < dim || (residual && residual_stride < dim) || (sum && sum_stride < dim) || (y && y_stride < dim))
+            return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_layer_norm: stride below dim");
+        if (q) {
+            rc = check_q8(ctx, "mqg_layer_norm", q_stride, q_type, group, scale, scale_stride, dim);
+            if (rc != MQG_OK) return rc;
+        }
+        return mqg::run_layer_norm(ctx, x, x_stride, residual, residual_stride, weight, bias, eps, num_rows_dev, cap_rows, dim, dtype, sum, sum_stride,
+                                   y, y_stride, q, q_stride, q_type, group, scale, scale_stride, static_cast<hipStream_t>(stream));
+    });
+}
+
+int mqg_layer_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, const void *sum, int64_t sum_stride, const float *weight,
+                          const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows_dev, int64_t cap_rows, int32_t dim,
+                          int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, float *grad_bias, mqg_stream stream) {
+    if (!ctx) return MQG_ERR_INVALID_ARG;
+    return guarded([&]() -> int {
+        int rc = check_norm_rows(ctx, "mqg_layer_norm_backward", cap_rows, dim, dtype, eps);
+        if (rc != MQG_OK) return rc;
+        if (cap_rows > 0 && (!grad_y || !sum || !grad_x)) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_layer_norm_backward: NULL grad_y, sum or grad_x");
+        if (gy_stride < dim || sum_stride < dim || gx_stride < dim || (grad_sum && gs_stride < dim))
+            return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_layer_norm_backward: stride below dim");
+        return mqg::run_layer_norm_backward(ctx, grad_y, gy_stride, sum, sum_stride, weight, grad_sum, gs_stride, eps, num_rows_dev, cap_rows, dim,
+                                          dtype, grad_x, gx_stride, grad_weight, grad_bias, static_cast<hipStream_t>(stream));
+    });
+}
+
 int mqg_sage_mean_aggregate_q8(mqg_ctx *ctx, const mqg_block *block, const void *q, int64_t q_stride, int32_t q_type, int32_t group,
                                const float *scale, int64_t scale_stride, void *out, int64_t out_stride, int32_t dim, int32_t dtype,
                                mqg_stream stream) {
@@ -786,13 +843,74 @@ int mqg_muon_step(mqg_ctx *ctx, const mqg_matrices *grad, const mqg_matrices *mo
     });
 }
 
+static int check_param_list(mqg_ctx *ctx, const char *who, const mqg_param *params, int32_t num) {
+    if (num < 0 || (num > 0 && !params)) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": negative num_params or NULL params");
+    for (int32_t i = 0; i < num; ++i) {
+        const mqg_param &p = params[i];
+        if (p.numel < 0) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": negative numel");
+        if (p.grad && !valid_layer_dtype(p.grad_type)) return fail(ctx, MQG_ERR_INVALID_ARG, std::string(who) + ": bad grad_type");
+    }
+    return MQG_OK;
+}
+
+int mqg_grad_norm(mqg_ctx *ctx, const mqg_param *params, int32_t num_params, float mul, float max_norm, float *norm, float *scale,
+                  mqg_stream stream) {
+    if (!ctx) return MQG_ERR_INVALID_ARG;
+    return guarded([&]() -> int {
+        int rc = check_param_list(ctx, "mqg_grad_norm", params, num_params);
+        if (rc != MQG_OK) return rc;
+        if (!norm && !scale) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_grad_norm: neither norm nor scale is given");
+        if (!(mul > 0.f) || std::isinf(mul)) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_grad_norm: mul is not a positive number");
+        if (!(max_norm > 0.f)) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_grad_norm: max_norm is not positive");
+        return mqg::run_grad_norm(ctx, params, num_params, mul, max_norm, norm, scale, static_cast<hipStream_t>(stream));
+    });
+}
+
+int mqg_adamw_step(mqg_ctx *ctx, const mqg_param *params, int32_t num_params, const mqg_adamw *plan, mqg_stream stream) {
+    if (!ctx) return MQG_ERR_INVALID_ARG;
+    return guarded([&]() -> int {
+        int rc = check_param_list(ctx, "mqg_adamw_step", params, num_params);
+        if (rc != MQG_OK) return rc;
+        if (!plan) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: NULL plan");
+        if (!std::isfinite(plan->lr) || !std::isfinite(plan->weight_decay))
+            return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: lr or weight_decay is not finite");
+        if (!(plan->beta1 >= 0.0 && plan->beta1 < 1.0 && plan->beta2 >= 0.0 && plan->beta2 < 1.0))
+            return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: beta1 or beta2 is outside 0..1");
+        if (!(plan->eps >= 0.0) || std::isinf(plan->eps)) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: eps is negative or not a number");
+        if (!plan->step_dev && plan->step < 1) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: step below 1");
+        for (int32_t i = 0; i < num_params; ++i) {
+            const mqg_param &p = params[i];
+            if (!p.grad || p.numel == 0) continue;
+            if (!valid_layer_dtype(p.weight_type) || (p.copy && !valid_layer_dtype(p.copy_type)))
+                return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: bad weight_type or copy_type");
+            if (p.state_type != MQG_STATE_F32 && p.state_type != MQG_STATE_E4M3) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: bad state_type");
+            if (!p.weight || !p.m || !p.v) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: NULL weight, m or v");
+            if (p.state_type == MQG_STATE_E4M3 && (!p.m_scale || !p.v_scale)) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: NULL m_scale or v_scale");
+            if (!std::isfinite(p.lr_scale) || !std::isfinite(p.decay_scale))
+                return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: lr_scale or decay_scale is not finite");
+        }
+        auto bytes = [](int32_t dtype) { return dtype == MQG_F32 ? 4 : 2; };
+        auto state = [](const mqg_param &p) { return p.numel * (p.state_type == MQG_STATE_E4M3 ? 1 : 4); };
+        auto scales = [](const mqg_param &p) { return mqg::ceil_div(p.numel, MQG_ADAMW_BLOCK) * 4; };
+        using Range = std::pair<const void *, int64_t>;
+        if (overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.weight, p.numel * bytes(p.weight_type)); }) ||
+            overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.copy, p.numel * bytes(p.copy_type)); }) ||
+            overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.m, state(p)); }) ||
+            overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.v, state(p)); }) ||
+            overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.state_type == MQG_STATE_E4M3 ? p.m_scale : nullptr, scales(p)); }) ||
+            overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.state_type == MQG_STATE_E4M3 ? p.v_scale : nullptr, scales(p)); }))
+            return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: two tensors share a weight, copy, moment or scale");
+        return mqg::run_adamw_step(ctx, params, num_params, plan, static_cast<hipStream_t>(stream));
+    });
+}
+
 int mqg_ctx_reserve_layer(mqg_ctx *ctx, int32_t norm_dim, int32_t num_mats, int32_t rows, int32_t cols) {
     if (!ctx) return MQG_ERR_INVALID_ARG;
     return guarded([&]() -> int {
         if (norm_dim < 0 || num_mats < 0 || rows < 0 || cols < 0) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_ctx_reserve_layer: negative size");
         if (norm_dim > MQG_NORM_MAX_DIM || num_mats > MQG_ORTH_MAX_MATS || rows > MQG_ORTH_MAX_SIDE || cols > MQG_ORTH_MAX_SIDE)
             return fail(ctx, MQG_ERR_UNSUPPORTED, "mqg_ctx_reserve_layer: above the calls' limits");
-        return mqg::reserve_layer_scratch(ctx, std::max(mqg::norm_scratch_bytes(norm_dim), mqg::orth_scratch_bytes(num_mats, rows, cols)),
+        return mqg::reserve_layer_scratch(ctx, std::max(mqg::layer_norm_scratch_bytes(norm_dim), mqg::orth_scratch_bytes(num_mats, rows, cols)),
                                           "mqg_ctx_reserve_layer");
     });
 }

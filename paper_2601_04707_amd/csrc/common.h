@@ -18,6 +18,8 @@ constexpr int kWavesPerBlock = kBlock / kWave;
 constexpr int kBitmapTileWords = 1024;   // the frontier bitmap is padded to a multiple of this many words
 constexpr int kCandidates = 256;         // per-wavefront candidate slots of the threshold selection
 
+constexpr int kGradNormParts = 1024;     // workgroups of a gradients' norm at most
+
 // Graphs of up to this many bitmap tiles of kBlock words (3 M nodes): in sampling, the launch that lists new sources records
 // their rows, and the launch that samples the next block relabels the one before, which takes three bitmaps and places for two
 // blocks' neighbours.  Every tile with hubs adds to the list's count, one after the other, 13 ns each: above, the row information
@@ -117,6 +119,7 @@ struct mqg_ctx {
     int64_t cache_arena_bytes = 0;
     // what the calls of a layer leave between their launches (norm.hip, orthogonal.hip); grows with the calls, or by mqg_ctx_reserve_layer
     mqg::Arena layer_scratch;
+    double *norm_parts = nullptr;        // [kGradNormParts] sums of squares of the workgroups of a gradients' norm (adamw.hip)
     // hash-table dedup (MQG_OPT_DEDUP_HASH); allocated when the option is first used
     bool dedup_hash = false;
     unsigned long long *hash_table = nullptr;      // [hash_capacity] (id << 32 | position), all ones = empty
@@ -201,7 +204,7 @@ int run_select_row_candidates(mqg_ctx *ctx, const uint64_t *keys, const uint32_t
                               int32_t prioritised, int32_t ordered, uint32_t *out_mask, hipStream_t s);
 int run_exp_tickets(mqg_ctx *ctx, uint64_t seed, int64_t tag, int64_t first, int64_t n, uint64_t *tickets, hipStream_t s);
 int run_set_sampling_priority(mqg_ctx *ctx, const mqg_graph *g, const mqg_cache *cache, hipStream_t s);
-// the calls of a layer (norm.hip, aggregate_q8.hip, orthogonal.hip)
+// the calls of a layer (norm.hip, layer_norm.hip, aggregate_q8.hip, orthogonal.hip, adamw.hip)
 int ensure_layer_scratch(mqg_ctx *ctx, int64_t bytes, hipStream_t s, const char *who);
 int reserve_layer_scratch(mqg_ctx *ctx, int64_t bytes, const char *who);
 int64_t norm_scratch_bytes(int32_t dim);
@@ -212,6 +215,15 @@ int run_rms_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *resi
 int run_rms_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, const void *sum, int64_t sum_stride, const float *weight,
                           const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows, int64_t cap_rows, int32_t dim,
                           int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, hipStream_t s);
+int64_t layer_norm_scratch_bytes(int32_t dim);
+int run_layer_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const float *weight, const float *bias,
+                   float eps, const int64_t *num_rows, int64_t cap_rows, int32_t dim, int32_t dtype, void *sum, int64_t sum_stride, void *y,
+                   int64_t y_stride, void *q, int64_t q_stride, int32_t q_type, int32_t group, float *scale, int64_t scale_stride, hipStream_t s);
+int run_layer_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, const void *sum, int64_t sum_stride, const float *weight,
+                            const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows, int64_t cap_rows, int32_t dim,
+                            int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, float *grad_bias, hipStream_t s);
+int run_grad_norm(mqg_ctx *ctx, const mqg_param *params, int32_t num, float mul, float most, float *norm, float *scale, hipStream_t s);
+int run_adamw_step(mqg_ctx *ctx, const mqg_param *params, int32_t num, const mqg_adamw *plan, hipStream_t s);
 int run_mean_aggregate_q8(mqg_ctx *ctx, const mqg_block *b, const void *q, int64_t q_stride, int32_t q_type, int32_t group, const float *scale,
                           int64_t scale_stride, void *out, int64_t out_stride, int32_t dim, int32_t dtype, hipStream_t s);
 struct OrthCall {

@@ -1,0 +1,529 @@
+// Layer norm of the rows between two layers, with the residual's addition and an output in 8 bits, and its backward.
+//
+//   forward    s = x + r,  d = s - mean(s),  y = d R w + b with R = 1/sqrt(mean(d^2) + eps),  8 bits as of the root-mean-square norm
+//   backward   with u = d R and h = gy w:  gx = R (h - mean(h) - u mean(h u)) + gs,  gw = sum over rows of gy u,  gb = sum over rows of gy
+//
+// Both are bound by memory: every input is read once and every output written once, a row stays in registers in between, laid out over lanes as the other
+// norm's rows are.  The mean is taken first and the squares are those of the differences from it, so that rows whose mean is large against their
+// spread keep it; what the mean was off by (the differences' own mean, which the same exchange gives) is taken out of both.
+#include <algorithm>
+
+#include "norm_rows.h"
+
+namespace mqg {
+
+int64_t layer_norm_scratch_bytes(int32_t dim) { return int64_t(kNormParts) * 2 * dim * int64_t(sizeof(float)); }
+
+namespace {
+
+struct LayerArgs {
+    const void *x, *residual;
+    const float *weight, *bias;
+    const int64_t *num_rows;
+    void *sum, *y;
+    uint8_t *q;
+    float *scale;
+    int64_t x_stride, residual_stride, sum_stride, y_stride, q_stride, scale_stride;
+    int64_t cap_rows;
+    float eps;
+    int32_t dim, q_type, group;       // group: columns per scale, 0 = the row
+};
+
+// Sums and maxima that the lanes of a row find together, MOST at a time.  Rows of several wavefronts exchange through LDS: two buffers in turn, so that one
+// barrier per exchange is enough (who writes a buffer again has passed the barrier behind which all have read it).
+template <int LANES, int MOST>
+struct RowExchange {
+    static constexpr int kWaves = LANES / kWave;
+    static constexpr int kRoom = LANES > kWave ? 2 * MOST * kWaves : 1;
+    float *lds;
+    int turn = 0;
+    __device__ __forceinline__ explicit RowExchange(float *l) : lds(l) {}
+    template <int N>
+    __device__ __forceinline__ void sums(float (&v)[N]) {
+        static_assert(N <= MOST, "room for MOST values of every wavefront");
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i], LANES < kWave ? LANES : kWave);
+        if constexpr (LANES > kWave) {
+            float *buf = lds + turn * MOST * kWaves;
+            turn ^= 1;
+            if (lane_id() == 0) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) buf[N * (threadIdx.x >> 6) + i] = v[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = buf[i];
+#pragma unroll
+            for (int k = 1; k < kWaves; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] += buf[N * k + i];
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = of_wave<LANES>(v[i]);
+    }
+    __device__ __forceinline__ uint32_t max(uint32_t v) {
+        v = lanes_max(v, LANES < kWave ? LANES : kWave);
+        if constexpr (LANES > kWave) {
+            float *buf = lds + turn * MOST * kWaves;
+            turn ^= 1;
+            if (lane_id() == 0) buf[threadIdx.x >> 6] = __uint_as_float(v);
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) v = max_u32(v, __float_as_uint(buf[k]));
+        }
+        return v;
+    }
+};
+
+// A lane's vectors of a row, and which of their elements are its own: bit j of own[k].
+template <int LANES, int NV, int V>
+struct RowPlaces {
+    Span<V> at[NV];
+    uint32_t own[NV];
+    static constexpr uint32_t kAll = (1u << V) - 1;
+    __device__ __forceinline__ RowPlaces(int lane, int dim) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            at[k] = Span<V>(k * LANES + lane, dim);
+            own[k] = 0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) own[k] |= at[k].mine(j) && at[k].base + j < dim ? 1u << j : 0u;
+        }
+    }
+    // Others' elements become zero.
+    __device__ __forceinline__ void keep_own(float (&v)[NV][V]) const {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (own[k] != kAll) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[k][j] = (own[k] >> j) & 1 ? v[k][j] : 0.f;
+            }
+    }
+};
+
+template <int NV, int V>
+__device__ __forceinline__ float lane_sum(const float (&v)[NV][V]) {
+    float all = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        float part = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) part += v[k][j];
+        all += part;
+    }
+    return all;
+}
+template <int NV, int V>
+__device__ __forceinline__ float lane_dot(const float (&x)[NV][V], const float (&y)[NV][V]) {
+    float all = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        float part = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) part += x[k][j] * y[k][j];
+        all += part;
+    }
+    return all;
+}
+
+template <int V>
+__device__ __forceinline__ void load_bias(const float *b, const Span<V> &at, int dim, float (&out)[V]) {
+    if (b) {
+        load_weight(b, at, dim, out);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) out[j] = 0.f;
+    }
+}
+
+// The variance of differences d from a mean that is off by their own mean c.  (A variance that is no number stays none.)
+__device__ __forceinline__ float variance(float sum, float squares, int dim, float *c) {
+    const float n = static_cast<float>(dim);
+    *c = sum / n;
+    const float var = squares / n - *c * *c;
+    return var < 0.f ? 0.f : var;
+}
+// Rows that are taken again: the variance may have lost terms at either end of 32 bits' range, or the mean was off by as much as the row spreads (a row of
+// equal values is off by its mean's rounding, and spreads not at all).  Then the differences are formed from the row's first value, exactly where they are small against it,
+// times two powers of two: (s low - s0 low) high.  |s| up to 2^128 becomes up to 2^48, and variances of 2^100 and more 2^-60 and more; spreads of 2^-149 to 2^-50 become
+// 2^-59 to 2^40.
+struct Unit {
+    float low, high;
+};
+__device__ __forceinline__ bool odd_row(float var, float eps, float c) { return odd_mean(var + eps) || c * c > var; }
+__device__ __forceinline__ Unit odd_unit(float mean) {
+    return mean < 0x1p-100f ? Unit{1.f, 0x1p+90f} : mean <= 0x1p+100f ? Unit{1.f, 1.f} : Unit{0x1p-80f, 1.f};
+}
+// The variance of the row times unit, and eps, or infinity, whose factor is 0, where the row's own factor is above 32 bits' numbers: rows of equal values without an
+// epsilon, and such as spread less than 2^-128.
+__device__ __forceinline__ float unit_variance(float var, float eps, float unit) {
+    const float v = var + eps * unit * unit;
+    return sqrtf(v) < unit * 0x1p-128f || v == 0.f ? __uint_as_float(0x7F800000u) : v;
+}
+
+template <typename T, int LANES, int NV, bool PAST>
+__global__ void __launch_bounds__(LANES > kBlock ? LANES : kBlock)
+k_layer_norm(LayerArgs a) {
+    constexpr int V = Vec<T>::kLen;
+    constexpr int kThreads = LANES > kBlock ? LANES : kBlock;
+    constexpr int kRows = kThreads / LANES;                // rows of a workgroup
+    using Exchange = RowExchange<LANES, 2>;
+    __shared__ float lds[Exchange::kRoom];
+    Exchange lanes(lds);
+    const int lane = static_cast<int>(threadIdx.x) % LANES;
+    const int64_t n = rows_of(a.num_rows, a.cap_rows);
+    const int dim = a.dim;
+    const float top = a.q_type == MQG_Q_E4M3 ? 448.f : 127.f;
+    const int group_lanes = a.group / V;                   // lanes that share a scale, 0 = the row's
+    const RowPlaces<LANES, NV, V> places(lane, dim);
+    float w[NV][V], b[NV][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        load_weight(a.weight, places.at[k], dim, w[k]);
+        load_bias(a.bias, places.at[k], dim, b[k]);
+    }
+    for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; row < n; row += int64_t(gridDim.x) * kRows) {
+        using W = typename Vec<T>::Whole;
+        const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+        const T *r0 = static_cast<const T *>(a.residual) + row * a.residual_stride;
+        float d[NV][V];
+        auto read = [&]() __attribute__((always_inline)) {
+            W raw[NV], more[NV];
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                raw[k] = load_span(x, places.at[k], dim);
+                if (a.residual) more[k] = load_span(r0, places.at[k], dim);
+            }
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    d[k][j] = static_cast<float>(raw[k][j]);
+                    if (a.residual) d[k][j] += static_cast<float>(more[k][j]);
+                }
+        };
+        float c = 0.f;
+        // d becomes its values less their mean, but for c
+        auto centre = [&]() __attribute__((always_inline)) {
+            places.keep_own(d);
+            float mean[1] = {lane_sum(d)};
+            lanes.sums(mean);
+            mean[0] /= static_cast<float>(dim);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) d[k][j] -= mean[0];
+            places.keep_own(d);
+            float both[2] = {lane_sum(d), lane_dot(d, d)};
+            lanes.sums(both);
+            return variance(both[0], both[1], dim, &c);
+        };
+        read();
+        float s[NV][V];
+        if (a.sum) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) s[k][j] = d[k][j];
+        }
+        float var = centre();
+        float mean = var + a.eps;
+        if (odd_row(var, a.eps, c)) {                      // (the same in all lanes of a row; nothing of the row is written yet, which may be in its input's place)
+            float s0 = static_cast<float>(x[0]);
+            if (a.residual) s0 += static_cast<float>(r0[0]);
+            const Unit u = odd_unit(mean);
+            read();
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) d[k][j] = (d[k][j] * u.low - s0 * u.low) * u.high;
+            var = centre();
+            mean = unit_variance(var, a.eps, u.low * u.high);
+        }
+        const float r = 1.0f / sqrtf(mean);
+        if (a.sum) {
+            T *sum = static_cast<T *>(a.sum) + row * a.sum_stride;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) store_span<PAST>(sum, places.at[k], dim, s[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) d[k][j] = fmaf((d[k][j] - c) * r, w[k][j], b[k][j]);
+        if (a.y) {
+            T *y = static_cast<T *>(a.y) + row * a.y_stride;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) store_span<PAST>(y, places.at[k], dim, d[k]);
+        }
+        if (!a.q) continue;
+        uint8_t *q = a.q + row * a.q_stride;
+        float *scale = a.scale + row * a.scale_stride;
+        places.keep_own(d);
+        uint32_t most[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            most[k] = 0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) most[k] = max_u32(most[k], __float_as_uint(d[k][j]) & 0x7FFFFFFFu);
+        }
+        if (group_lanes == 0) {
+            uint32_t m = most[0];
+#pragma unroll
+            for (int k = 1; k < NV; ++k) m = max_u32(m, most[k]);
+            const Scale sc = scale_of(lanes.max(m), 1.f, top);
+            if (lane == 0) scale[0] = sc.scale;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) store_q(q, places.at[k], dim, d[k], sc, a.q_type);
+        } else {
+            const int width = group_lanes < LANES ? group_lanes : LANES;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const Scale sc = scale_of(lanes_max(most[k], width), 1.f, top);
+                const int i = k * LANES + lane;
+                if (lane % width == 0 && i * V < dim) scale[i / group_lanes] = sc.scale;
+                store_q(q, places.at[k], dim, d[k], sc, a.q_type);
+            }
+        }
+    }
+}
+
+struct LayerGradArgs {
+    const void *grad_y, *s, *grad_sum;
+    const float *weight;
+    const int64_t *num_rows;
+    void *grad_x;
+    float *weight_parts, *bias_parts;      // every workgroup's share of the two gradients, `pitch` apart; null if not wanted
+    int64_t gy_stride, s_stride, gs_stride, gx_stride, pitch;
+    int64_t cap_rows;
+    float eps;
+    int32_t dim;
+};
+
+template <typename T, int LANES, int NV, bool PAST>
+__global__ void __launch_bounds__(LANES > kBlock ? LANES : kBlock)
+k_layer_norm_backward(LayerGradArgs a) {
+    using W = typename Vec<T>::Whole;
+    constexpr int V = Vec<T>::kLen;
+    constexpr int kThreads = LANES > kBlock ? LANES : kBlock;
+    constexpr int kRows = kThreads / LANES;
+    constexpr int kCols = LANES * NV * V;
+    using Exchange = RowExchange<LANES, 3>;
+    // rows of several wavefronts: their exchange; others: the wavefronts' sums of the two gradients
+    __shared__ float lds[LANES > kWave ? Exchange::kRoom : kWavesPerBlock * kCols];
+    Exchange lanes(lds);
+    const int lane = static_cast<int>(threadIdx.x) % LANES;
+    const int64_t n = rows_of(a.num_rows, a.cap_rows);
+    const int dim = a.dim;
+    const RowPlaces<LANES, NV, V> places(lane, dim);
+    float w[NV][V], gw[NV][V], gb[NV][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        load_weight(a.weight, places.at[k], dim, w[k]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) gw[k][j] = gb[k][j] = 0.f;
+    }
+    struct Row {
+        W s[NV], g[NV], gs[NV];
+    };
+    auto load = [&](int64_t row) __attribute__((always_inline)) {
+        Row v;
+        const T *sr = static_cast<const T *>(a.s) + row * a.s_stride;
+        const T *gr = static_cast<const T *>(a.grad_y) + row * a.gy_stride;
+        const T *gs = static_cast<const T *>(a.grad_sum) + row * a.gs_stride;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            v.s[k] = load_span(sr, places.at[k], dim);
+            v.g[k] = load_span(gr, places.at[k], dim);
+            if (a.grad_sum) v.gs[k] = load_span(gs, places.at[k], dim);
+        }
+        return v;
+    };
+    // A row is on its way while the one before is worked on, if the registers hold both.
+    constexpr bool kAhead = kThreads < 1024 || NV * V < 16;
+    const int64_t step = int64_t(gridDim.x) * kRows;
+    int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES;
+    Row next;
+    if (kAhead && row < n) next = load(row);
+    for (; row < n; row += step) {
+        const Row v = kAhead ? next : load(row);
+        if (kAhead && row + step < n) next = load(row + step);
+        places.keep_own(w);                                // (here a row's loads are on their way: before, they would wait for the weight's)
+        float d[NV][V], g[NV][V], h[NV][V];
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                d[k][j] = static_cast<float>(v.s[k][j]);
+                g[k][j] = static_cast<float>(v.g[k][j]);
+            }
+        places.keep_own(g);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) h[k][j] = g[k][j] * w[k][j];
+        float c = 0.f, dot = 0.f, h_mean = 0.f;
+        // d becomes its values less their mean, but for c; dot the mean of d h, h_mean that of h
+        auto centre = [&]() __attribute__((always_inline)) {
+            places.keep_own(d);
+            float first[2] = {lane_sum(d), lane_sum(h)};
+            lanes.sums(first);
+            first[0] /= static_cast<float>(dim);
+            h_mean = first[1] / static_cast<float>(dim);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) d[k][j] -= first[0];
+            places.keep_own(d);
+            float then[3] = {lane_sum(d), lane_dot(d, d), lane_dot(d, h)};
+            lanes.sums(then);
+            const float var = variance(then[0], then[1], dim, &c);
+            dot = then[2] / static_cast<float>(dim) - c * h_mean;
+            return var;
+        };
+        float var = centre(), unit = 1.f;
+        float mean = var + a.eps;
+        if (odd_row(var, a.eps, c)) {
+            const float s0 = static_cast<float>(*(static_cast<const T *>(a.s) + row * a.s_stride));
+            const Unit u = odd_unit(mean);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) d[k][j] = (static_cast<float>(v.s[k][j]) * u.low - s0 * u.low) * u.high;
+            unit = u.low * u.high;
+            var = centre();
+            mean = unit_variance(var, a.eps, unit);
+        }
+        const float r = 1.0f / sqrtf(mean);                // of d; the row's is r unit
+        dot *= r;
+        T *gx = static_cast<T *>(a.grad_x) + row * a.gx_stride;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float out[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float u = (d[k][j] - c) * r;
+                gw[k][j] += g[k][j] * u;
+                gb[k][j] += g[k][j];
+                out[j] = r * unit * (h[k][j] - h_mean - u * dot);
+                if (a.grad_sum) out[j] += static_cast<float>(v.gs[k][j]);
+            }
+            store_span<PAST>(gx, places.at[k], dim, out);
+        }
+    }
+    // The workgroup's share of a gradient.
+    auto put = [&](float *parts, float (&v)[NV][V]) __attribute__((always_inline)) {
+        if (!parts) return;
+        float *part = parts + int64_t(blockIdx.x) * a.pitch;
+        if constexpr (LANES > kWave) {                     // the workgroup is one row's: nothing to join
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if ((places.own[k] >> j) & 1) part[places.at[k].base + j] = v[k][j];
+        } else {
+            const int wave = static_cast<int>(threadIdx.x) >> 6;
+            __syncthreads();                               // the other gradient's sums are read
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    float x = v[k][j];
+#pragma unroll
+                    for (int off = LANES; off < kWave; off <<= 1) x += __shfl_xor(x, off, kWave);
+                    if (lane_id() < LANES && ((places.own[k] >> j) & 1)) lds[wave * kCols + places.at[k].base + j] = x;
+                }
+            __syncthreads();
+            for (int col = static_cast<int>(threadIdx.x); col < dim; col += kThreads) {
+                float x = lds[col];
+#pragma unroll
+                for (int k = 1; k < kWavesPerBlock; ++k) x += lds[k * kCols + col];
+                part[col] = x;
+            }
+        }
+    };
+    put(a.weight_parts, gw);
+    put(a.bias_parts, gb);
+}
+
+template <typename T>
+int launch_layer_norm(mqg_ctx *ctx, const LayerArgs &a, hipStream_t s) {
+    const RowShape sh = row_shape(a.dim, Vec<T>::kLen, a.cap_rows);
+    const int64_t cells = a.cap_rows * a.dim, arrays = 1 + (a.residual != nullptr) + (a.sum != nullptr) + (a.y != nullptr);
+    const bool past = cells * (arrays * int64_t(sizeof(T)) + (a.q != nullptr)) >= kPastBytes;
+    const int threads = std::max(sh.lanes, kBlock);
+    const int64_t most = sizeof(T) == 4 ? (int64_t(1) << 31) - 1 : int64_t(8192) * kBlock / threads;
+    const int64_t grid = std::min<int64_t>(std::min<int64_t>(ceil_div(a.cap_rows, threads / sh.lanes), most), ((int64_t(1) << 32) - 1) / threads);
+#define MQG_GO(T, L, N)                                                                                                            \
+    do {                                                                                                                           \
+        if (past) MQG_LAUNCH(ctx, "k_layer_norm", s, (k_layer_norm<T, L, N, true><<<static_cast<uint32_t>(grid), threads, 0, s>>>(a)));  \
+        else MQG_LAUNCH(ctx, "k_layer_norm", s, (k_layer_norm<T, L, N, false><<<static_cast<uint32_t>(grid), threads, 0, s>>>(a)));      \
+    } while (0)
+    MQG_NORM_SHAPES(T, MQG_GO)
+#undef MQG_GO
+    return MQG_OK;
+}
+
+template <typename T>
+int launch_layer_norm_backward(mqg_ctx *ctx, LayerGradArgs a, float *grad_weight, float *grad_bias, hipStream_t s) {
+    const RowShape sh = row_shape(a.dim, Vec<T>::kLen, a.cap_rows);
+    const int threads = std::max(sh.lanes, kBlock);
+    const int64_t sets = ceil_div(a.cap_rows, threads / sh.lanes);
+    const int wanted = (grad_weight != nullptr) + (grad_bias != nullptr);
+    // Rows of a few rounds are one workgroup's, whose sums are the gradients, and the second launch falls away.
+    const bool alone = wanted && sets > 0 && sets <= (sh.lanes <= kBlock ? 4 : 2);
+    const int grid = alone ? 1 : static_cast<int>(std::min<int64_t>(sets, kNormParts));
+    const bool past = a.cap_rows * a.dim * (a.grad_sum ? 4 : 3) * int64_t(sizeof(T)) >= kPastBytes;
+    a.pitch = int64_t(wanted) * a.dim;
+    float *parts = nullptr;
+    if (alone) {
+        a.weight_parts = grad_weight;
+        a.bias_parts = grad_bias;
+    } else if (wanted) {
+        int rc = ensure_layer_scratch(ctx, layer_norm_scratch_bytes(a.dim), s, "mqg_layer_norm_backward");
+        if (rc != MQG_OK) return rc;
+        parts = reinterpret_cast<float *>(ctx->layer_scratch.data);
+        a.weight_parts = grad_weight ? parts : nullptr;
+        a.bias_parts = grad_bias ? parts + (grad_weight ? a.dim : 0) : nullptr;
+    }
+#define MQG_GO(T, L, N)                                                                                                                  \
+    do {                                                                                                                                 \
+        if (past) MQG_LAUNCH(ctx, "k_layer_norm_backward", s, (k_layer_norm_backward<T, L, N, true><<<grid, threads, 0, s>>>(a)));            \
+        else MQG_LAUNCH(ctx, "k_layer_norm_backward", s, (k_layer_norm_backward<T, L, N, false><<<grid, threads, 0, s>>>(a)));                \
+    } while (0)
+    if (grid > 0) {
+        MQG_NORM_SHAPES(T, MQG_GO)
+    }
+#undef MQG_GO
+    if (wanted && !alone) {
+        const int cols = wanted * a.dim;
+        MQG_LAUNCH(ctx, "k_sum_parts", s,
+                   (k_sum_parts<<<static_cast<int>(ceil_div(cols, kSumCols)), kSumThreads, 0, s>>>(parts, grid, cols, grad_weight ? grad_weight : grad_bias,
+                                                                                                    a.dim, grad_bias)));
+    }
+    return MQG_OK;
+}
+
+}  // namespace
+
+int run_layer_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const float *weight, const float *bias,
+                   float eps, const int64_t *num_rows, int64_t cap_rows, int32_t dim, int32_t dtype, void *sum, int64_t sum_stride, void *y,
+                   int64_t y_stride, void *q, int64_t q_stride, int32_t q_type, int32_t group, float *scale, int64_t scale_stride, hipStream_t s) {
+    if (cap_rows == 0) return MQG_OK;
+    const LayerArgs a{x, residual, weight, bias, num_rows, sum, y, static_cast<uint8_t *>(q), scale, x_stride, residual_stride, sum_stride,
+                      y_stride, q_stride, scale_stride, cap_rows, eps, dim, q_type, group};
+    if (dtype == MQG_F16) return launch_layer_norm<F16>(ctx, a, s);
+    if (dtype == MQG_BF16) return launch_layer_norm<BF16>(ctx, a, s);
+    return launch_layer_norm<float>(ctx, a, s);
+}
+
+int run_layer_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, const void *sum, int64_t sum_stride, const float *weight,
+                            const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows, int64_t cap_rows, int32_t dim,
+                            int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, float *grad_bias, hipStream_t s) {
+    const LayerGradArgs a{grad_y, sum, grad_sum, weight, num_rows, grad_x, nullptr, nullptr, gy_stride, sum_stride, gs_stride, gx_stride, 0, cap_rows,
+                          eps, dim};
+    if (dtype == MQG_F16) return launch_layer_norm_backward<F16>(ctx, a, grad_weight, grad_bias, s);
+    if (dtype == MQG_BF16) return launch_layer_norm_backward<BF16>(ctx, a, grad_weight, grad_bias, s);
+    return launch_layer_norm_backward<float>(ctx, a, grad_weight, grad_bias, s);
+}
+
+}  // namespace mqg

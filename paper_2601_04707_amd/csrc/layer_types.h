@@ -1,10 +1,12 @@
-// Element types, 16-byte vectors and wavefront reductions of the kernels of a layer (norm.hip, aggregate_q8.hip, orthogonal.hip).
+// Element types, 16-byte vectors, wavefront reductions and the way to 8 bits of the kernels of a layer (norm.hip, layer_norm.hip, aggregate_q8.hip, orthogonal.hip,
+// adamw.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include "device_utils.h"
+#include "mqg.h"
 
 namespace mqg {
 
@@ -137,6 +139,54 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v, int width) {
     if (width > 16) v = max_u32(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 16, kWave)));
     if (width > 32) v = max_u32(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 32, kWave)));
     return v;
+}
+
+// How a group is taken to 8 bits, from z = s w and the row's r, y = z r.  Values and scale have r in common, so q = z / (max|z| / top) has two roundings before
+// its own and r's is none of them (of a million e4m3 values 0.4 to 0.7 are the neighbour of the one that the formula has in 64 bits, of int8 1.5 to 2; of y divided
+// by its scale in 32 bits 0.7 to 0.9 and 2 to 2.2); where that quotient would leave 32 bits' range, or the scale is the least one, q = y / scale.
+// most: the largest |z|'s bit pattern (patterns of absolute values order as the values do, with infinity and NaN above all others): a group that
+// holds a value that is not finite has the scale NaN, so that all its values read NaN.
+struct Scale {
+    float scale, by, div;             // q = (z by) / div
+};
+__device__ __forceinline__ Scale scale_of(uint32_t most, float r, float top) {
+    const float t = __uint_as_float(most) / top, scale = t * r;
+    if (!(scale < __uint_as_float(0x7F800000u))) {
+        const float nan = __uint_as_float(0x7FC00000u);
+        return {nan, nan, nan};
+    }
+    if (!(scale > 0x1p-126f)) return {0x1p-126f, r, 0x1p-126f};
+    return t > 0x1p-100f ? Scale{scale, 1.f, t} : Scale{scale, r, scale};
+}
+
+// V values in 8 bits, four to a word.
+template <int V>
+__device__ __forceinline__ void to_8bit(const float (&z)[V], const Scale &s, int q_type, uint32_t (&w)[V / 4]) {
+    const float inv = 1.0f / s.div;
+    float y[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {                          // the quotient by the reciprocal, and its remainder's
+        const float num = z[j] * s.by, quot = num * inv;
+        y[j] = fmaf(fmaf(-quot, s.div, num), inv, quot);
+    }
+    if (q_type == MQG_Q_E4M3) {
+#pragma unroll
+        for (int k = 0; k < V / 4; ++k) {
+            int p = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k], y[4 * k + 1], 0, false);
+            w[k] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2], y[4 * k + 3], p, true));
+        }
+    } else {
+        const bool number = s.scale == s.scale;
+#pragma unroll
+        for (int k = 0; k < V / 4; ++k) {
+            w[k] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int v = number ? static_cast<int>(rintf(y[4 * k + j])) : 0;
+                w[k] |= (static_cast<uint32_t>(v) & 0xFFu) << (8 * j);
+            }
+        }
+    }
 }
 
 }  // namespace mqg

@@ -13,11 +13,9 @@
 #include <algorithm>
 
 #include "common.h"
-#include "layer_types.h"
+#include "norm_rows.h"
 
 namespace mqg {
-
-constexpr int kNormParts = 512;      // workgroups of a backward at most
 
 int64_t norm_scratch_bytes(int32_t dim) { return int64_t(kNormParts) * dim * int64_t(sizeof(float)); }
 
@@ -35,32 +33,6 @@ struct NormArgs {
     float eps;
     int32_t dim, q_type, group;       // group: columns per scale, 0 = the row
 };
-
-__device__ __forceinline__ int64_t rows_of(const int64_t *num_rows, int64_t cap) {
-    if (!num_rows) return cap;
-    const int64_t n = *num_rows;
-    return n < cap ? (n > 0 ? n : 0) : cap;
-}
-
-// The mean of squares and eps of a row outside this range: its sums may have lost terms at either end of 32 bits' range, and so may the square of the factor
-// R = 1/sqrt(mean).  They are taken again of s times a power of two, row_unit, after which they are well inside (large: |s| up to 2^128 becomes up to 2^56, sums
-// up to 2^126; small, where eps doesn't make up for the lost terms: 2^-149 to 2^-43 become 2^-59 to 2^47).  Rows of fp16 never need it but for zeros.
-// The comparison costs the others nothing to 1.5 % (300,000 x 100 fp32 66.9 -> 67.8 us).
-__device__ __forceinline__ bool odd_mean(float mean) {
-    return __float_as_uint(mean) - __float_as_uint(0x1p-100f) > __float_as_uint(0x1p+100f) - __float_as_uint(0x1p-100f);
-}
-__device__ __forceinline__ float row_unit(float mean) { return mean > 0x1p+100f ? 0x1p-72f : mean < 0x1p-100f ? 0x1p+90f : 1.f; }
-// The mean of s times unit, or infinity, whose factor is 0, where the row's own factor, unit times as large, is above 32 bits' numbers: zeros without an epsilon,
-// and rows whose root mean square is below 2^-128.
-__device__ __forceinline__ float unit_mean(float squares, int dim, float eps, float unit) {
-    const float mean = squares / static_cast<float>(dim) + eps * unit * unit;
-    return sqrtf(mean) < unit * 0x1p-128f ? __uint_as_float(0x7F800000u) : mean;
-}
-// What is the same in all lanes of a wavefront, for the compiler, too: scalar registers
-template <int LANES>
-__device__ __forceinline__ float of_wave(float v) {
-    return LANES < kWave ? v : __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
-}
 
 // What the lanes of a row find together.  Rows of several wavefronts exchange through LDS: two buffers in turn, so that one barrier
 // per exchange is enough (who writes a buffer again has passed the barrier behind which all have read it).
@@ -115,70 +87,6 @@ struct RowLanes {
         return v;
     }
 };
-
-// How a group is taken to 8 bits, from z = s w and the row's r, y = z r.  Values and scale have r in common, so q = z / (max|z| / top) has two roundings before
-// its own and r's is none of them (of a million e4m3 values 0.4 to 0.7 are the neighbour of the one that the formula has in 64 bits, of int8 1.5 to 2; of y divided
-// by its scale in 32 bits 0.7 to 0.9 and 2 to 2.2); where that quotient would leave 32 bits' range, or the scale is the least one, q = y / scale.
-// most: the largest |z|'s bit pattern (patterns of absolute values order as the values do, with infinity and NaN above all others): a group that
-// holds a value that is not finite has the scale NaN, so that all its values read NaN.
-struct Scale {
-    float scale, by, div;             // q = (z by) / div
-};
-__device__ __forceinline__ Scale scale_of(uint32_t most, float r, float top) {
-    const float t = __uint_as_float(most) / top, scale = t * r;
-    if (!(scale < __uint_as_float(0x7F800000u))) {
-        const float nan = __uint_as_float(0x7FC00000u);
-        return {nan, nan, nan};
-    }
-    if (!(scale > 0x1p-126f)) return {0x1p-126f, r, 0x1p-126f};
-    return t > 0x1p-100f ? Scale{scale, 1.f, t} : Scale{scale, r, scale};
-}
-
-// V values of a row in 8 bits
-template <int V>
-__device__ __forceinline__ void store_q(uint8_t *row, const Span<V> &at, int dim, const float (&z)[V], const Scale &s, int q_type) {
-    const float inv = 1.0f / s.div;
-    float y[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {                          // the quotient by the reciprocal, and its remainder's
-        const float num = z[j] * s.by, quot = num * inv;
-        y[j] = fmaf(fmaf(-quot, s.div, num), inv, quot);
-    }
-    uint32_t w[V / 4];
-    if (q_type == MQG_Q_E4M3) {
-#pragma unroll
-        for (int k = 0; k < V / 4; ++k) {
-            int p = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k], y[4 * k + 1], 0, false);
-            w[k] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2], y[4 * k + 3], p, true));
-        }
-    } else {
-        const bool number = s.scale == s.scale;
-#pragma unroll
-        for (int k = 0; k < V / 4; ++k) {
-            w[k] = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int v = number ? static_cast<int>(rintf(y[4 * k + j])) : 0;
-                w[k] |= (static_cast<uint32_t>(v) & 0xFFu) << (8 * j);
-            }
-        }
-    }
-    if (at.skip == 0 && dim >= V) {
-        typedef uint32_t Words __attribute__((ext_vector_type(V / 4)));
-        typedef Words AnyWords __attribute__((aligned(1)));
-        Words v;
-#pragma unroll
-        for (int k = 0; k < V / 4; ++k) {
-            if constexpr (V == 4) v = w[k];
-            else v[k] = w[k];
-        }
-        *reinterpret_cast<AnyWords *>(row + at.base) = v;
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (at.mine(j) && at.base + j < dim) row[at.base + j] = static_cast<uint8_t>(w[j / 4] >> (8 * (j % 4)));
-    }
-}
 
 template <typename T, int LANES, int NV, bool PAST>
 __global__ void __launch_bounds__(LANES > kBlock ? LANES : kBlock)
@@ -461,81 +369,6 @@ k_rms_norm_backward(NormGradArgs a) {
     }
 }
 
-// out[c] = sum over the parts, 16 columns a workgroup: 64 threads take a column's parts in turn, eight of them on their way together, and their sums are
-// added in order.
-constexpr int kSumCols = 16, kSumThreads = 1024;
-__global__ void __launch_bounds__(kSumThreads)
-k_sum_parts(const float *__restrict__ parts, int num_parts, int dim, float *__restrict__ out) {
-    constexpr int kTurns = kSumThreads / kSumCols, kAhead = 8;
-    __shared__ float lds[kTurns][kSumCols + 1];
-    const int c = static_cast<int>(blockIdx.x) * kSumCols + static_cast<int>(threadIdx.x) % kSumCols;
-    const int turn = static_cast<int>(threadIdx.x) / kSumCols;
-    float v = 0.f;
-    if (c < dim)
-        for (int p0 = turn; p0 < num_parts; p0 += kAhead * kTurns) {
-            float x[kAhead];
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) x[k] = p0 + k * kTurns < num_parts ? parts[int64_t(p0 + k * kTurns) * dim + c] : 0.f;
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) v += x[k];
-        }
-    lds[turn][threadIdx.x % kSumCols] = v;
-    __syncthreads();
-    // the 64 sums of a column by the lanes of a wavefront
-    const int col = static_cast<int>(threadIdx.x) / kWave;
-    v = lanes_sum(lds[lane_id()][col], kWave);
-    if (lane_id() == 0 && static_cast<int>(blockIdx.x) * kSumCols + col < dim) out[static_cast<int>(blockIdx.x) * kSumCols + col] = v;
-}
-static_assert(kSumThreads / kSumCols == kWave && kSumThreads / kWave == kSumCols, "a wavefront adds a column");
-
-// How a row is laid out: lanes, and vectors per lane.  As few lanes as hold it with up to four vectors each within a wavefront; longer rows have a
-// workgroup of 512 (8,192 rows of 8,192 bf16: 109 us and the backward 112; 256 lanes 144 and 112, 1,024 126 and 120), the longest one of 1,024.
-// Few rows are spread as wide as they go: there is nothing else to do.
-struct RowShape {
-    int lanes, nv;
-};
-constexpr int kFewRows = 256;
-RowShape row_shape(int dim, int vec, int64_t rows) {
-    const int vecs = static_cast<int>(ceil_div(dim, vec));
-    for (int lanes = 4; lanes <= kWave; lanes <<= 1)
-        if (vecs <= lanes) return {lanes, 1};
-    if (rows <= kFewRows) {
-        if (vecs <= 256) return {256, 1};
-        if (vecs > 512 && vecs <= 1024) return {1024, 1};
-    }
-    if (vecs <= 4 * kWave) return {kWave, static_cast<int>(ceil_div(vecs, kWave))};
-    if (vecs <= 2 * 512) return {512, static_cast<int>(ceil_div(vecs, 512))};
-    return {1024, vecs <= 2 * 1024 ? 2 : 4};
-}
-
-#define MQG_NORM_SHAPES(T, GO)                                     \
-    switch (sh.lanes) {                                            \
-        case 4: GO(T, 4, 1); break;                                \
-        case 8: GO(T, 8, 1); break;                                \
-        case 16: GO(T, 16, 1); break;                              \
-        case 32: GO(T, 32, 1); break;                              \
-        case 64:                                                   \
-            if (sh.nv == 1) GO(T, 64, 1);                          \
-            else if (sh.nv == 2) GO(T, 64, 2);                     \
-            else if (sh.nv == 3) GO(T, 64, 3);                     \
-            else GO(T, 64, 4);                                     \
-            break;                                                 \
-        case 256: GO(T, 256, 1); break;                            \
-        case 512:                                                  \
-            if (sh.nv == 1) GO(T, 512, 1);                         \
-            else GO(T, 512, 2);                                    \
-            break;                                                 \
-        default:                                                   \
-            if (sh.nv == 1) GO(T, 1024, 1);                        \
-            else if (sh.nv == 2) GO(T, 1024, 2);                   \
-            else if constexpr (sizeof(T) == 4) GO(T, 1024, 4);     \
-    }
-
-// A call that moves twice what the chip's memory-side cache holds leaves little of its own output there: that goes past the caches (109,000 x 602
-// fp32 rows, four times 262 MB: 202 -> 190 us; 295,000 x 256 bf16, four times 151 MB: 112 -> 97; backward of these 194 -> 191 and 111 -> 108).  Smaller ones
-// keep it for the next reader, though they would be faster by themselves, too (40,000 x 1,000 bf16, 320 MB: 55 -> 49; 60,000 x 256 fp32 42 -> 37).
-constexpr int64_t kPastBytes = int64_t(512) << 20;
-
 template <typename T>
 int launch_norm(mqg_ctx *ctx, const NormArgs &a, hipStream_t s) {
     const RowShape sh = row_shape(a.dim, Vec<T>::kLen, a.cap_rows);
@@ -587,10 +420,9 @@ int launch_norm_backward(mqg_ctx *ctx, NormGradArgs a, float *grad_weight, hipSt
 #undef MQG_GO
     if (grad_weight && !alone)
         MQG_LAUNCH(ctx, "k_sum_parts", s,
-                   (k_sum_parts<<<static_cast<int>(ceil_div(a.dim, kSumCols)), kSumThreads, 0, s>>>(a.parts, grid, a.dim, grad_weight)));
+                   (k_sum_parts<<<static_cast<int>(ceil_div(a.dim, kSumCols)), kSumThreads, 0, s>>>(a.parts, grid, a.dim, grad_weight, a.dim, nullptr)));
     return MQG_OK;
 }
-#undef MQG_NORM_SHAPES
 
 }  // namespace
 

@@ -3,7 +3,7 @@
 The four operations keep the names of the C ABI (``include/mqg.h``):
 ``mqg_build_cache``, ``mqg_sample_blocks``, ``mqg_gather_features`` and
 ``mqg_sage_mean_aggregate``, and so do the calls of a layer (``mqg_rms_norm``,
-``mqg_muon_step`` and those between them in this file).  Torch is used for device memory, pinned host
+``mqg_adamw_step`` and those between them in this file).  Torch is used for device memory, pinned host
 memory and streams; every step of the path runs in the library's kernels.
 There is no fallback: if the shared library is missing, importing this module
 raises.
@@ -23,6 +23,7 @@ MQG_OK, MQG_ERR_INVALID_ARG, MQG_ERR_CAPACITY, MQG_ERR_HIP, MQG_ERR_UNSUPPORTED 
 MQG_F32, MQG_F16, MQG_BF16 = 0, 1, 2
 MQG_Q_E4M3, MQG_Q_INT8 = 0, 1
 MQG_NORM_MAX_DIM = 16384
+MQG_STATE_F32, MQG_STATE_E4M3, MQG_ADAMW_BLOCK = 0, 1, 128
 MQG_ORTH_MAX_STEPS, MQG_ORTH_MAX_SIDE, MQG_ORTH_MAX_MATS = 32, 65536, 65535
 MQG_I32, MQG_I64 = 0, 1
 MQG_OPT_FORCE_SLOW_SELECT, MQG_OPT_PROFILE, MQG_OPT_MISS_INFLIGHT_BYTES, MQG_OPT_HEAVY_DEGREE, MQG_OPT_DEDUP_HASH = 1, 2, 3, 4, 5
@@ -40,7 +41,7 @@ EXPORTS = [
     "mqg_select_smallest_keys", "mqg_select_row_candidates", "mqg_sample_blocks_seed_dev",
     "mqg_gather_features_static", "mqg_exp_tickets", "mqg_gather_features_cached", "mqg_gather_features_missed",
     "mqg_ctx_reserve", "mqg_ctx_reserve_layer", "mqg_rms_norm", "mqg_rms_norm_backward", "mqg_sage_mean_aggregate_q8",
-    "mqg_orthogonalize", "mqg_muon_step",
+    "mqg_orthogonalize", "mqg_muon_step", "mqg_layer_norm", "mqg_layer_norm_backward", "mqg_grad_norm", "mqg_adamw_step",
 ]
 
 if not os.path.exists(LIB_PATH):
@@ -81,6 +82,17 @@ class CMatrices(ctypes.Structure):
 
 class COrth(ctypes.Structure):
     _fields_ = [("steps", _i32), ("eps", ctypes.c_float), ("coeffs", ctypes.POINTER(ctypes.c_float))]
+
+
+class CParam(ctypes.Structure):
+    _fields_ = [("numel", _i64), ("weight", _vp), ("grad", _vp), ("copy", _vp), ("m", _vp), ("v", _vp), ("m_scale", _vp), ("v_scale", _vp),
+                ("weight_type", _i32), ("grad_type", _i32), ("copy_type", _i32), ("state_type", _i32), ("lr_scale", ctypes.c_float),
+                ("decay_scale", ctypes.c_float)]
+
+
+class CAdamw(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", _i64), ("step_dev", _vp), ("lr_dev", _vp), ("grad_scale_dev", _vp)]
 
 
 lib.mqg_version.restype = _i32
@@ -155,6 +167,15 @@ lib.mqg_rms_norm.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _f32, _vp, _i64, _i
                              _i64, _vp]
 lib.mqg_rms_norm_backward.restype = ctypes.c_int
 lib.mqg_rms_norm_backward.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _f32, _vp, _i64, _i32, _i32, _vp, _i64, _vp, _vp]
+lib.mqg_layer_norm.restype = ctypes.c_int
+lib.mqg_layer_norm.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _vp, _f32, _vp, _i64, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _vp,
+                               _i64, _vp]
+lib.mqg_layer_norm_backward.restype = ctypes.c_int
+lib.mqg_layer_norm_backward.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _f32, _vp, _i64, _i32, _i32, _vp, _i64, _vp, _vp, _vp]
+lib.mqg_grad_norm.restype = ctypes.c_int
+lib.mqg_grad_norm.argtypes = [_vp, ctypes.POINTER(CParam), _i32, _f32, _f32, _vp, _vp, _vp]
+lib.mqg_adamw_step.restype = ctypes.c_int
+lib.mqg_adamw_step.argtypes = [_vp, ctypes.POINTER(CParam), _i32, ctypes.POINTER(CAdamw), _vp]
 lib.mqg_sage_mean_aggregate_q8.restype = ctypes.c_int
 lib.mqg_sage_mean_aggregate_q8.argtypes = [_vp, ctypes.POINTER(CBlock), _vp, _i64, _i32, _i32, _vp, _i64, _vp, _i64, _i32, _i32, _vp]
 lib.mqg_orthogonalize.restype = ctypes.c_int
@@ -260,7 +281,7 @@ class Context:
         self.check(lib.mqg_ctx_reserve(self.h, what, layerwise_rows))
 
     def reserve_layer(self, norm_dim: int = 0, num_mats: int = 0, rows: int = 0, cols: int = 0):
-        """Allocate now the scratch of a layer's calls: mqg_rms_norm_backward for rows of up to norm_dim columns,
+        """Allocate now the scratch of a layer's calls: mqg_rms_norm_backward and mqg_layer_norm_backward for rows of up to norm_dim columns,
         mqg_orthogonalize and mqg_muon_step for stacks of num_mats matrices of rows x cols."""
         self.check(lib.mqg_ctx_reserve_layer(self.h, norm_dim, num_mats, rows, cols))
 
@@ -652,6 +673,44 @@ def mqg_rms_norm_backward(ctx: Context, grad_y: torch.Tensor, s: torch.Tensor, w
                                         shape[0], shape[1], _layer_dtype(s), grad_x.data_ptr(), gxs, _ptr(grad_weight), _stream(stream)))
 
 
+def mqg_layer_norm(ctx: Context, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+                   residual: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                   q: Optional[torch.Tensor] = None, q_scale: Optional[torch.Tensor] = None, group: int = 0, eps: float = 1e-5,
+                   num_rows: Optional[torch.Tensor] = None, stream=None) -> None:
+    """y = (s - mean) / sqrt(variance + eps) * weight + bias of s = x + residual, row by row; the other arguments as mqg_rms_norm's."""
+    shape, dtype = x.shape, x.dtype
+    assert x.dim() == 2
+    xs = _rows(x, dtype, shape)
+    rs = _rows(residual, dtype, shape) if residual is not None else 0
+    ss = _rows(sum_out, dtype, shape) if sum_out is not None else 0
+    ys = _rows(y, dtype, shape) if y is not None else 0
+    _norm_inputs(weight, num_rows, shape[1])
+    _norm_inputs(bias, None, shape[1])
+    qs = qt = cs = 0
+    if q is not None:
+        qt, qs, cs = _q_type(q), _rows(q, q.dtype, shape), _scales(q, q_scale, group, shape)
+    ctx.check(lib.mqg_layer_norm(ctx.h, x.data_ptr(), xs, _ptr(residual), rs, _ptr(weight), _ptr(bias), eps, _ptr(num_rows), shape[0], shape[1],
+                                 _layer_dtype(x), _ptr(sum_out), ss, _ptr(y), ys, _ptr(q), qs, qt, group, _ptr(q_scale) if q is not None else None, cs,
+                                 _stream(stream)))
+
+
+def mqg_layer_norm_backward(ctx: Context, grad_y: torch.Tensor, s: torch.Tensor, weight: Optional[torch.Tensor], grad_x: torch.Tensor, *,
+                            grad_weight: Optional[torch.Tensor] = None, grad_bias: Optional[torch.Tensor] = None,
+                            grad_sum: Optional[torch.Tensor] = None, eps: float = 1e-5, num_rows: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradient of mqg_layer_norm at the stored sum s (x where there was no residual): grad_x, the same for x and residual, grad_weight
+    and grad_bias ([dim] float32, written).  grad_sum: the gradient that reaches s by its other uses."""
+    shape, dtype = s.shape, s.dtype
+    assert s.dim() == 2
+    ss, gys, gxs = _rows(s, dtype, shape), _rows(grad_y, dtype, shape), _rows(grad_x, dtype, shape)
+    gss = _rows(grad_sum, dtype, shape) if grad_sum is not None else 0
+    _norm_inputs(weight, num_rows, shape[1])
+    _norm_inputs(grad_weight, None, shape[1])
+    _norm_inputs(grad_bias, None, shape[1])
+    ctx.check(lib.mqg_layer_norm_backward(ctx.h, grad_y.data_ptr(), gys, s.data_ptr(), ss, _ptr(weight), _ptr(grad_sum), gss, eps, _ptr(num_rows),
+                                          shape[0], shape[1], _layer_dtype(s), grad_x.data_ptr(), gxs, _ptr(grad_weight), _ptr(grad_bias),
+                                          _stream(stream)))
+
+
 def mqg_sage_mean_aggregate_q8(ctx: Context, blocks, l: int, q: torch.Tensor, q_scale: torch.Tensor, out: torch.Tensor, *, group: int = 0,
                                stream=None) -> None:
     """mqg_sage_mean_aggregate of source rows in 8 bits with scales, as mqg_rms_norm writes them; out: float32, float16 or bfloat16."""
@@ -699,6 +758,96 @@ def mqg_muon_step(ctx: Context, grad: torch.Tensor, momentum: torch.Tensor, weig
     g, m, w, p = _matrices(grad), _matrices(momentum), _matrices(weight), _orth(steps, coeffs, eps)
     ctx.check(lib.mqg_muon_step(ctx.h, ctypes.byref(g), ctypes.byref(m), ctypes.byref(w), lr, beta, int(nesterov), weight_decay, scale,
                                 ctypes.byref(p), _stream(stream)))
+
+
+class Params:
+    """The tensors that mqg_adamw_step steps and whose gradients mqg_grad_norm reads: made once, kept by the program.
+
+    weights, grads: lists of contiguous tensors of the same shapes (a gradient of None: the tensor is left alone); without weights the list
+    serves mqg_grad_norm only.  m, v: the moments, zeros of state_dtype if not given - float32, or float8_e4m3fn (v: its root) with
+    m_scale, v_scale, a float32 per MQG_ADAMW_BLOCK elements.  copies: tensors that receive the weights rounded to their type.
+    lr_scale, decay_scale: a number for every tensor."""
+
+    def __init__(self, weights=None, grads=None, *, m=None, v=None, m_scale=None, v_scale=None, copies=None, state_dtype=torch.float32,
+                 lr_scale=None, decay_scale=None):
+        assert weights is not None or grads is not None
+        like = weights if weights is not None else grads
+        n = len(like)
+        eight = (m[0].dtype if m else state_dtype) == torch.float8_e4m3fn
+        if weights is not None:
+            assert (m is None) == (v is None)
+            if m is None:
+                m, v = ([torch.zeros(w.shape, dtype=state_dtype, device=w.device) for w in weights] for _ in range(2))
+            if eight and m_scale is None and v_scale is None:
+                m_scale, v_scale = ([torch.zeros(-(-w.numel() // MQG_ADAMW_BLOCK), device=w.device) for w in weights] for _ in range(2))
+        self.weights, self.copies, self.m, self.v, self.m_scale, self.v_scale = weights, copies, m, v, m_scale, v_scale
+        self.c = (CParam * n)()
+        for given in (m, v, copies, lr_scale, decay_scale) + ((m_scale, v_scale) if eight else ()):
+            assert given is None or len(given) == n, "one of each for every tensor"
+        for i, p in enumerate(self.c):
+            p.lr_scale, p.decay_scale = lr_scale[i] if lr_scale else 1.0, decay_scale[i] if decay_scale else 1.0
+            if like[i] is None:
+                continue
+            p.numel = like[i].numel()
+            if weights is None:
+                continue
+            p.weight, p.weight_type = self._data(weights[i], like[i].shape), _layer_dtype(weights[i])
+            if copies is not None and copies[i] is not None:
+                p.copy, p.copy_type = self._data(copies[i], like[i].shape), _layer_dtype(copies[i])
+            state = torch.float8_e4m3fn if eight else torch.float32
+            p.m, p.v, p.state_type = self._data(m[i], like[i].shape, state), self._data(v[i], like[i].shape, state), int(eight)
+            if eight:
+                blocks = (-(-p.numel // MQG_ADAMW_BLOCK),)
+                p.m_scale, p.v_scale = self._data(m_scale[i], blocks, torch.float32), self._data(v_scale[i], blocks, torch.float32)
+        self.grads = None
+        if grads is not None:
+            self.set_grads(grads)
+
+    @staticmethod
+    def _data(t: torch.Tensor, shape, dtype=None) -> int:
+        assert t.is_cuda and t.is_contiguous() and t.shape == shape and (dtype is None or t.dtype is dtype), \
+            f"expected {tuple(shape)} of {dtype or t.dtype}, contiguous on the GPU, got {tuple(t.shape)} of {t.dtype}"
+        return t.data_ptr()
+
+    def set_grads(self, grads) -> None:
+        """The gradients of the steps that follow."""
+        assert len(grads) == len(self.c)
+        for i, (p, g) in enumerate(zip(self.c, grads)):
+            if g is None:
+                p.grad = None
+            else:
+                p.grad, p.grad_type = self._data(g, self.weights[i].shape if self.weights is not None else g.shape), _layer_dtype(g)
+                p.numel = g.numel()
+        self.grads = list(grads)
+
+
+def _one(t, dtype) -> Optional[int]:
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype is dtype and t.numel() >= 1
+    return t.data_ptr()
+
+
+def mqg_grad_norm(ctx: Context, params: Params, *, max_norm: float = float("inf"), mul: float = 1.0, norm: Optional[torch.Tensor] = None,
+                  scale: Optional[torch.Tensor] = None, stream=None) -> None:
+    """norm = mul * the norm of all gradients, scale = mul * min(1, max_norm / norm): float32 tensors on the GPU, either may be None."""
+    ctx.check(lib.mqg_grad_norm(ctx.h, params.c, len(params.c), mul, max_norm, _one(norm, torch.float32), _one(scale, torch.float32), _stream(stream)))
+
+
+def mqg_adamw_step(ctx: Context, params: Params, *, lr, step, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                   weight_decay: float = 0.01, grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
+    """An AdamW step of all tensors.  lr: a number, or a float32 tensor on the GPU; step: 1, 2, ..., or an int64 tensor on the GPU, read when the step
+    runs; grad_scale: a float32 tensor on the GPU that the gradients are multiplied by (mqg_grad_norm's scale)."""
+    plan = CAdamw(beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay, grad_scale_dev=_one(grad_scale, torch.float32))
+    if isinstance(lr, torch.Tensor):
+        plan.lr_dev = _one(lr, torch.float32)
+    else:
+        plan.lr = lr
+    if isinstance(step, torch.Tensor):
+        plan.step_dev = _one(step, torch.int64)
+    else:
+        plan.step = step
+    ctx.check(lib.mqg_adamw_step(ctx.h, params.c, len(params.c), ctypes.byref(plan), _stream(stream)))
 
 
 def mqg_queue_size(max_prepare_ms: float, mean_compute_ms: float, total_mem_bytes: int, peak_mem_bytes: int,
