@@ -18,7 +18,7 @@ constexpr int kWavesPerBlock = kBlock / kWave;
 constexpr int kBitmapTileWords = 1024;   // the frontier bitmap is padded to a multiple of this many words
 constexpr int kCandidates = 256;         // per-wavefront candidate slots of the threshold selection
 
-constexpr int kGradNormParts = 1024;     // workgroups of a gradients' norm at most
+constexpr int kGradNormParts = 2048;     // workgroups of a gradients' norm at most
 
 // Graphs of up to this many bitmap tiles of kBlock words (3 M nodes): in sampling, the launch that lists new sources records
 // their rows, and the launch that samples the next block relabels the one before, which takes three bitmaps and places for two
@@ -119,7 +119,7 @@ struct mqg_ctx {
     int64_t cache_arena_bytes = 0;
     // what the calls of a layer leave between their launches (norm.hip, orthogonal.hip); grows with the calls, or by mqg_ctx_reserve_layer
     mqg::Arena layer_scratch;
-    double *norm_parts = nullptr;        // [kGradNormParts] sums of squares of the workgroups of a gradients' norm (adamw.hip)
+    double *norm_parts = nullptr;        // [kGradNormParts + 1] sums of squares of the workgroups of a gradients' norm, and how many have theirs (adamw.hip)
     // hash-table dedup (MQG_OPT_DEDUP_HASH); allocated when the option is first used
     bool dedup_hash = false;
     unsigned long long *hash_table = nullptr;      // [hash_capacity] (id << 32 | position), all ones = empty

@@ -119,6 +119,19 @@ __device__ __forceinline__ uint32_t dpp_u32(uint32_t v) {
     return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, 0xF, 0xF, true));
 }
 
+// What a lane and the one 16 (32) lanes from it have, the lower one's first, in both of them.
+struct Pair {
+    uint32_t x, y;
+};
+__device__ __forceinline__ Pair swap_rows(uint32_t v) {
+    const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return {p[0], p[1]};
+}
+__device__ __forceinline__ Pair swap_halves(uint32_t v) {
+    const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return {p[0], p[1]};
+}
+
 // Sum over `width` neighbouring lanes (a power of two, the same in all lanes of the wavefront), the same in each of them:
 // the two halves of every step are added in either order, so no lane rounds otherwise than another.
 __device__ __forceinline__ float lanes_sum(float v, int width) {
@@ -126,8 +139,14 @@ __device__ __forceinline__ float lanes_sum(float v, int width) {
     if (width > 2) v += dpp_f32<0x4E>(v);                  // lanes 2 3 0 1
     if (width > 4) v += dpp_f32<0x141>(v);                 // a half row of eight, mirrored
     if (width > 8) v += dpp_f32<0x140>(v);                 // a row of 16, mirrored
-    if (width > 16) v += __shfl_xor(v, 16, kWave);
-    if (width > 32) v += __shfl_xor(v, 32, kWave);
+    if (width > 16) {
+        const Pair p = swap_rows(__float_as_uint(v));
+        v = __uint_as_float(p.x) + __uint_as_float(p.y);
+    }
+    if (width > 32) {
+        const Pair p = swap_halves(__float_as_uint(v));
+        v = __uint_as_float(p.x) + __uint_as_float(p.y);
+    }
     return v;
 }
 __device__ __forceinline__ uint32_t max_u32(uint32_t a, uint32_t b) { return a > b ? a : b; }
@@ -136,8 +155,14 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v, int width) {
     if (width > 2) v = max_u32(v, dpp_u32<0x4E>(v));
     if (width > 4) v = max_u32(v, dpp_u32<0x141>(v));
     if (width > 8) v = max_u32(v, dpp_u32<0x140>(v));
-    if (width > 16) v = max_u32(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 16, kWave)));
-    if (width > 32) v = max_u32(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 32, kWave)));
+    if (width > 16) {
+        const Pair p = swap_rows(v);
+        v = max_u32(p.x, p.y);
+    }
+    if (width > 32) {
+        const Pair p = swap_halves(v);
+        v = max_u32(p.x, p.y);
+    }
     return v;
 }
 
