@@ -50,6 +50,13 @@ __host__ __device__ __forceinline__ double power(double beta, int64_t t) {
     return all;
 }
 
+// How many elements before a tensor its first workgroup begins, so that each begins at a whole cache line of it.
+constexpr int kLine = 128;
+template <typename T>
+int line_shift(const T *p) {
+    return static_cast<int>(reinterpret_cast<uintptr_t>(p) % kLine / sizeof(T));
+}
+
 // What a launch of the step knows, 4 KB at most: a tensor's addresses (weight, gradient, m, v, then the copy and the scales if there are any),
 // its first workgroup, the elements of its last one, and which of a few pairs of factors it has.
 constexpr int kArgBytes = 4096, kFactors = 8;
@@ -79,20 +86,24 @@ enum { kWeight, kGrad, kM, kV };
 template <bool EIGHT, bool COPY>
 struct StepArgs {
     static constexpr int kCopy = 4, kMScale = 4 + COPY, kVScale = 5 + COPY, kPointers = 4 + COPY + 2 * EIGHT;
-    static constexpr int kTensors = (kArgBytes - static_cast<int>(sizeof(StepPlan)) - 16) / (6 * kPointers + 4 + 2 + 1);
+    static constexpr int kHigh = (kPointers + 1) / 2;
+    static constexpr int kTensors = (kArgBytes - static_cast<int>(sizeof(StepPlan))) / (4 * (kPointers + kHigh + 2));
+    // (whole words, which are read by scalar loads)
     StepPlan plan;
-    uint32_t low[kPointers][kTensors];   // addresses, of 48 bits
+    uint32_t low[kPointers][kTensors];   // addresses, of 48 bits; two of the high halves to a word
+    uint32_t high[kHigh][kTensors];
     uint32_t first[kTensors];
-    uint16_t high[kPointers][kTensors];
-    uint16_t last[kTensors];
-    uint8_t factor[kTensors];
+    uint32_t rest[kTensors];             // the last workgroup's elements less one, factors << 16, shift << 24 (of moments in 32 bits: blocks of 8-bit ones are counted from the tensor's beginning)
     void set(int which, int tensor, const void *p) {
         const uint64_t at = reinterpret_cast<uint64_t>(p);
+        const int by = which % 2 * 16;
+        uint32_t &h = high[which / 2][tensor];
         low[which][tensor] = static_cast<uint32_t>(at);
-        high[which][tensor] = static_cast<uint16_t>(at >> 32);
+        h = (h & ~(0xFFFFu << by)) | static_cast<uint32_t>(at >> 32 & 0xFFFF) << by;
     }
     __device__ __forceinline__ void *get(int which, int tensor) const {
-        return reinterpret_cast<void *>(static_cast<uint64_t>(high[which][tensor]) << 32 | low[which][tensor]);
+        const uint64_t at = static_cast<uint64_t>(high[which / 2][tensor] >> which % 2 * 16 & 0xFFFF) << 32 | low[which][tensor];
+        return (void *)reinterpret_cast<__attribute__((address_space(1))) void *>(at);      // (global memory's: the general kind of load waits for LDS, too)
     }
 };
 static_assert(sizeof(StepArgs<true, true>) <= kArgBytes && sizeof(StepArgs<true, false>) <= kArgBytes && sizeof(StepArgs<false, true>) <= kArgBytes &&
@@ -103,16 +114,16 @@ struct Some {
     typedef T Whole __attribute__((ext_vector_type(N)));
     typedef Whole Any __attribute__((aligned(sizeof(T))));
 };
-// N elements of a tensor from i on; zeros past its end.  FULL: they are all there; PAST: not to be kept in the caches, here and below
+// N elements of a tensor from i on, which may be below zero; zeros outside.  FULL: they are all there; PAST: not to be kept in the caches, here and below
 template <bool PAST, bool FULL, int N, typename T>
 __device__ __forceinline__ typename Some<T, N>::Whole load_some(const T *p, int64_t i, int64_t end) {
     typename Some<T, N>::Whole v;
-    if (FULL || i + N <= end) {
+    if (FULL || (i >= 0 && i + N <= end)) {
         if constexpr (PAST) v = __builtin_nontemporal_load(reinterpret_cast<const typename Some<T, N>::Any *>(p + i));
         else v = *reinterpret_cast<const typename Some<T, N>::Any *>(p + i);
     } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = i + j < end ? p[i + j] : static_cast<T>(0.f);
+        for (int j = 0; j < N; ++j) v[j] = i + j >= 0 && i + j < end ? p[i + j] : static_cast<T>(0.f);
     }
     return v;
 }
@@ -121,13 +132,13 @@ __device__ __forceinline__ void store_some(T *p, int64_t i, int64_t end, const f
     typename Some<T, N>::Whole v;
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = static_cast<T>(in[j]);
-    if (FULL || i + N <= end) {
+    if (FULL || (i >= 0 && i + N <= end)) {
         if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<typename Some<T, N>::Any *>(p + i));
         else *reinterpret_cast<typename Some<T, N>::Any *>(p + i) = v;
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j)
-            if (i + j < end) p[i + j] = v[j];
+            if (i + j >= 0 && i + j < end) p[i + j] = v[j];
     }
 }
 
@@ -137,12 +148,11 @@ struct Words {
     typedef uint32_t Whole __attribute__((ext_vector_type(W)));
     typedef Whole Any __attribute__((aligned(1)));
 };
-template <bool PAST, bool FULL, int E>
+template <bool FULL, int E>
 __device__ __forceinline__ typename Words<E / 4>::Whole load_8bit(const uint8_t *p, int64_t i, int64_t end) {
     typename Words<E / 4>::Whole w = 0;
     if (FULL || i + E <= end) {
-        if constexpr (PAST) w = __builtin_nontemporal_load(reinterpret_cast<const typename Words<E / 4>::Any *>(p + i));
-        else w = *reinterpret_cast<const typename Words<E / 4>::Any *>(p + i);
+        w = *reinterpret_cast<const typename Words<E / 4>::Any *>(p + i);
     } else {
 #pragma unroll
         for (int j = 0; j < E; ++j)
@@ -232,8 +242,8 @@ __device__ __forceinline__ void step_group(const StepNumbers &n, void *const (&o
         const int64_t i = base + k * kStepThreads * E;
         g_raw[k] = load_some<PAST, FULL, E>(grad, i, end);
         if constexpr (EIGHT) {
-            m8[k] = load_8bit<PAST, FULL, E>(static_cast<const uint8_t *>(of[kM]), i, end);
-            v8[k] = load_8bit<PAST, FULL, E>(static_cast<const uint8_t *>(of[kV]), i, end);
+            m8[k] = load_8bit<FULL, E>(static_cast<const uint8_t *>(of[kM]), i, end);
+            v8[k] = load_8bit<FULL, E>(static_cast<const uint8_t *>(of[kV]), i, end);
             ms[k] = FULL || i < end ? static_cast<const float *>(of[Args::kMScale])[i / MQG_ADAMW_BLOCK] : 0.f;
             vs[k] = FULL || i < end ? static_cast<const float *>(of[Args::kVScale])[i / MQG_ADAMW_BLOCK] : 0.f;
         } else {
@@ -317,12 +327,14 @@ k_adamw(StepArgs<EIGHT, COPY> a) {
     const StepPlan &p = a.plan;
     const int which = tensor_of<Args::kTensors>(a.first, p.count, blockIdx.x);
     const uint32_t first = a.first[which], next = which + 1 < p.count ? a.first[which + 1] : p.groups;
-    const int64_t end = int64_t(next - first - 1) * Shape::kGroup + a.last[which] + 1;
-    const int64_t group = int64_t(blockIdx.x - first) * Shape::kGroup;
+    const uint32_t rest = a.rest[which];
+    const int shift = EIGHT ? 0 : static_cast<int>(rest >> 24);
+    const int64_t end = int64_t(next - first - 1) * Shape::kGroup + static_cast<int>(rest & 0xFFFF) + 1 - shift;
+    const int64_t group = int64_t(blockIdx.x - first) * Shape::kGroup - shift;
     void *of[Args::kPointers];
 #pragma unroll
     for (int k = 0; k < Args::kPointers; ++k) of[k] = a.get(k, which);
-    StepFactors f = p.factors[a.factor[which]];
+    StepFactors f = p.factors[rest >> 16 & 0xFF];
     StepNumbers n{1.f, f.size, f.keep, p.beta1_f, p.beta2_f, p.new1, p.new2, p.root_by, p.eps, p.copy_type};
     if (p.grad_scale) {
         n.by = *p.grad_scale;
@@ -337,12 +349,12 @@ k_adamw(StepArgs<EIGHT, COPY> a) {
         n.root_by = debiased_root_by(p.beta2, step);
     }
     const int64_t base = group + static_cast<int>(threadIdx.x) * Shape::kElems;
-    if (group + Shape::kGroup <= end) step_group<TW, TG, EIGHT, COPY, PAST, true>(n, of, base, end);
+    if (group >= 0 && group + Shape::kGroup <= end) step_group<TW, TG, EIGHT, COPY, PAST, true>(n, of, base, end);
     else step_group<TW, TG, EIGHT, COPY, PAST, false>(n, of, base, end);
 }
 
 // What a launch of the norm knows: the tensors' gradients, their first chunks and the elements of their last ones.
-constexpr int kNormTensors = 280;
+constexpr int kNormTensors = 250;
 struct NormEnd {
     float mul, most;
     float *norm, *scale;
@@ -355,7 +367,7 @@ struct GradNormArgs {
     int32_t count, add;                  // add: workgroups that have a sum of the launch before
     const void *grad[kNormTensors];
     uint32_t first[kNormTensors];
-    uint16_t last[kNormTensors];
+    uint32_t rest[kNormTensors];         // the last chunk's elements less one, shift << 24
 };
 static_assert(sizeof(GradNormArgs) <= kArgBytes, "a launch's arguments");
 
@@ -388,12 +400,13 @@ k_grad_norm(GradNormArgs a) {
     for (uint32_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
         const int which = tensor_of<kNormTensors>(a.first, a.count, chunk);
         const uint32_t first = a.first[which], next = which + 1 < a.count ? a.first[which + 1] : a.chunks;
-        const int64_t end = int64_t(next - first - 1) * kNormChunk + a.last[which] + 1;
-        const int64_t base = int64_t(chunk - first) * kNormChunk;
+        const int shift = static_cast<int>(a.rest[which] >> 24);
+        const int64_t end = int64_t(next - first - 1) * kNormChunk + static_cast<int>(a.rest[which] & 0xFFFF) + 1 - shift;
+        const int64_t base = int64_t(chunk - first) * kNormChunk - shift;
         const T *grad = static_cast<const T *>(a.grad[which]);
         constexpr int V = Vec<T>::kLen, kLoads = kNormElems / V;
         typename Some<T, V>::Whole raw[kLoads];
-        if (base + kNormChunk <= end) {
+        if (base >= 0 && base + kNormChunk <= end) {
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) raw[k] = load_some<PAST, true, V>(grad, base + (k * kBlock + static_cast<int>(threadIdx.x)) * V, end);
         } else {
@@ -497,7 +510,7 @@ int step_tensors(mqg_ctx *ctx, const mqg_param *params, int32_t num, const StepP
         for (int64_t done = 0; done < p.numel;) {          // (parts are whole workgroups, and so whole blocks of 8-bit moments)
             int f = 0;
             while (f < factors && (a.plan.factors[f].lr_scale != p.lr_scale || a.plan.factors[f].decay_scale != p.decay_scale)) ++f;
-            if (a.plan.count == Args::kTensors || f == kFactors || a.plan.groups == kMostElems / kGroup) {
+            if (a.plan.count == Args::kTensors || f == kFactors || a.plan.groups >= kMostElems / kGroup) {
                 const int rc = launch();
                 if (rc != MQG_OK) return rc;
                 f = 0;
@@ -520,9 +533,9 @@ int step_tensors(mqg_ctx *ctx, const mqg_param *params, int32_t num, const StepP
                 a.set(Args::kVScale, at, p.v_scale + done / MQG_ADAMW_BLOCK);
             }
             a.first[at] = a.plan.groups;
-            a.last[at] = static_cast<uint16_t>((part - 1) % kGroup);
-            a.factor[at] = static_cast<uint8_t>(f);
-            a.plan.groups += static_cast<uint32_t>(ceil_div(part, kGroup));
+            const int shift = EIGHT ? 0 : line_shift(static_cast<TW *>(p.weight) + done);
+            a.rest[at] = static_cast<uint32_t>((part + shift - 1) % kGroup) | static_cast<uint32_t>(f) << 16 | static_cast<uint32_t>(shift) << 24;
+            a.plan.groups += static_cast<uint32_t>(ceil_div(part + shift, kGroup));
             done += part;
         }
     }
@@ -547,7 +560,7 @@ int run_grad_norm(mqg_ctx *ctx, const mqg_param *params, int32_t num, float mul,
             met = true;
             ++wanted;
             bytes += p.numel * type_size(type);
-            all_chunks += ceil_div(p.numel, kNormChunk);
+            all_chunks += ceil_div(p.numel + line_shift(static_cast<const char *>(p.grad)) / type_size(type), kNormChunk);
         }
         types += met;
     }
@@ -579,15 +592,17 @@ int run_grad_norm(mqg_ctx *ctx, const mqg_param *params, int32_t num, float mul,
             const mqg_param &p = params[i];
             if (!p.grad || p.grad_type != type) continue;
             for (int64_t done = 0; done < p.numel;) {
-                if (a.count == kNormTensors || a.chunks == kMostElems / kNormChunk) {
+                if (a.count == kNormTensors || a.chunks >= kMostElems / kNormChunk) {
                     const int rc = launch();
                     if (rc != MQG_OK) return rc;
                 }
                 const int64_t part = std::min(p.numel - done, (kMostElems / kNormChunk - a.chunks) * kNormChunk);
-                a.grad[a.count] = static_cast<const char *>(p.grad) + done * type_size(type);
-                a.last[a.count] = static_cast<uint16_t>((part - 1) % kNormChunk);
+                const char *grad = static_cast<const char *>(p.grad) + done * type_size(type);
+                const int shift = line_shift(grad) / type_size(type);
+                a.grad[a.count] = grad;
+                a.rest[a.count] = static_cast<uint32_t>((part + shift - 1) % kNormChunk) | static_cast<uint32_t>(shift) << 24;
                 a.first[a.count++] = a.chunks;
-                a.chunks += static_cast<uint32_t>(ceil_div(part, kNormChunk));
+                a.chunks += static_cast<uint32_t>(ceil_div(part + shift, kNormChunk));
                 done += part;
             }
         }
