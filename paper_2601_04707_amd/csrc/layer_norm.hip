@@ -12,7 +12,8 @@
 
 namespace mqg {
 
-int64_t layer_norm_scratch_bytes(int32_t dim) { return int64_t(kNormParts) * 2 * dim * int64_t(sizeof(float)); }
+// (rows of 2,048 columns and less may have 1,024 workgroups, others have 512: grad_parts)
+int64_t layer_norm_scratch_bytes(int32_t dim) { return std::max(std::min<int64_t>(dim, 2048) * 1024, int64_t(dim) * 512) * 2 * int64_t(sizeof(float)); }
 
 namespace {
 
@@ -25,7 +26,7 @@ struct LayerArgs {
     float *scale;
     int64_t x_stride, residual_stride, sum_stride, y_stride, q_stride, scale_stride;
     int64_t cap_rows;
-    float eps;
+    float eps, per_dim;               // per_dim: 1 / dim, by which means are taken (a division takes ten operations, in each of a row's lanes)
     int32_t dim, q_type, group;       // group: columns per scale, 0 = the row
 };
 
@@ -61,6 +62,15 @@ struct RowExchange {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = of_wave<LANES>(v[i]);
     }
+    // the first lane's, in all of them
+    __device__ __forceinline__ float first(float v) {
+        if constexpr (LANES <= kWave) return of_wave<LANES>(__shfl(v, lane_id() & ~(LANES - 1), kWave));
+        float *buf = lds + turn * MOST * kWaves;
+        turn ^= 1;
+        if (threadIdx.x == 0) buf[0] = v;
+        __syncthreads();
+        return buf[0];
+    }
     __device__ __forceinline__ uint32_t max(uint32_t v) {
         v = lanes_max(v, LANES < kWave ? LANES : kWave);
         if constexpr (LANES > kWave) {
@@ -90,6 +100,18 @@ struct RowPlaces {
             for (int j = 0; j < V; ++j) own[k] |= at[k].mine(j) && at[k].base + j < dim ? 1u << j : 0u;
         }
     }
+    // f(j) for the elements of vector k that are its own
+    template <typename F>
+    __device__ __forceinline__ void for_own(int k, F f) const {
+        if (own[k] == kAll) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) f(j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if ((own[k] >> j) & 1) f(j);
+        }
+    }
     // Others' elements become zero.
     __device__ __forceinline__ void keep_own(float (&v)[NV][V]) const {
 #pragma unroll
@@ -101,29 +123,40 @@ struct RowPlaces {
     }
 };
 
-template <int NV, int V>
-__device__ __forceinline__ float lane_sum(const float (&v)[NV][V]) {
-    float all = 0.f;
+// A thread's own sums, in registers, or, IN_LDS, in places of LDS that no other thread reads or writes: wide rows leave no registers for them.
+template <int NV, int V, int THREADS, bool IN_LDS>
+struct OwnSums {
+    typedef float Quad __attribute__((ext_vector_type(4)));
+    static constexpr int kQuads = IN_LDS ? NV * V / 4 * THREADS : 1;
+    float v[IN_LDS ? 1 : NV][V];
+    Quad *lds;
+    __device__ __forceinline__ explicit OwnSums(Quad *l) : lds(l + threadIdx.x) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        float part = 0.f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) part += v[k][j];
-        all += part;
+        for (int k = 0; k < NV; ++k) {
+            const float zeros[V] = {};
+            put(k, zeros);
+        }
     }
-    return all;
-}
-template <int NV, int V>
-__device__ __forceinline__ float lane_dot(const float (&x)[NV][V], const float (&y)[NV][V]) {
-    float all = 0.f;
+    __device__ __forceinline__ void get(int k, float (&out)[V]) const {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        float part = 0.f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) part += x[k][j] * y[k][j];
-        all += part;
+        for (int j = 0; j < V; ++j) out[j] = IN_LDS ? lds[(k * V / 4 + j / 4) * THREADS][j % 4] : v[IN_LDS ? 0 : k][j];
     }
-    return all;
+    __device__ __forceinline__ void put(int k, const float (&in)[V]) {
+        if constexpr (IN_LDS) {
+#pragma unroll
+            for (int h = 0; h < V / 4; ++h) lds[(k * V / 4 + h) * THREADS] = Quad{in[4 * h], in[4 * h + 1], in[4 * h + 2], in[4 * h + 3]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[k][j] = in[j];
+        }
+    }
+};
+
+// The compiler forms nothing of the vectors beforehand and keeps it: a row waits as it was loaded.
+template <typename W, int NV>
+__device__ __forceinline__ void as_loaded(W (&v)[NV]) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(v[k]));
 }
 
 template <int V>
@@ -136,12 +169,21 @@ __device__ __forceinline__ void load_bias(const float *b, const Span<V> &at, int
     }
 }
 
+// A mean, rounded: joined with the subtraction that follows it, it would be another one there than where it is used again.
+__device__ __forceinline__ float mean_of(float sum, float per_dim) {
+#pragma clang fp contract(off)
+    return sum * per_dim;
+}
 // The variance of differences d from a mean that is off by their own mean c.  (A variance that is no number stays none.)
-__device__ __forceinline__ float variance(float sum, float squares, int dim, float *c) {
-    const float n = static_cast<float>(dim);
-    *c = sum / n;
-    const float var = squares / n - *c * *c;
+__device__ __forceinline__ float variance(float sum, float squares, float per_dim, float *c) {
+    *c = mean_of(sum, per_dim);
+    const float var = squares * per_dim - *c * *c;
     return var < 0.f ? 0.f : var;
+}
+// One over the root of 2^-100 to 2^100, to one unit of its last place: the card's, and the rest of its error.
+__device__ __forceinline__ float reciprocal_root(float v) {
+    const float y = __builtin_amdgcn_rsqf(v);
+    return fmaf(y, 0.5f * fmaf(-v * y, y, 1.f), y);
 }
 // Rows that are taken again: the variance may have lost terms at either end of 32 bits' range, or the mean was off by as much as the row spreads (a row of
 // equal values is off by its mean's rounding, and spreads not at all).  Then the differences are formed from the row's first value, exactly where they are small against it,
@@ -182,89 +224,101 @@ k_layer_norm(LayerArgs a) {
         load_weight(a.weight, places.at[k], dim, w[k]);
         load_bias(a.bias, places.at[k], dim, b[k]);
     }
-    for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; row < n; row += int64_t(gridDim.x) * kRows) {
-        using W = typename Vec<T>::Whole;
+    using W = typename Vec<T>::Whole;
+    W raw[NV], more[NV];
+    constexpr bool kAhead = kThreads < 1024 || NV * V < 16;    // a row is on its way while the one before is worked on, if the registers hold both
+    auto load = [&](int64_t row) __attribute__((always_inline)) {
         const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
         const T *r0 = static_cast<const T *>(a.residual) + row * a.residual_stride;
-        float d[NV][V];
-        auto read = [&]() __attribute__((always_inline)) {
-            W raw[NV], more[NV];
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                raw[k] = load_span(x, places.at[k], dim);
-                if (a.residual) more[k] = load_span(r0, places.at[k], dim);
-            }
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    d[k][j] = static_cast<float>(raw[k][j]);
-                    if (a.residual) d[k][j] += static_cast<float>(more[k][j]);
-                }
-        };
-        float c = 0.f;
-        // d becomes its values less their mean, but for c
-        auto centre = [&]() __attribute__((always_inline)) {
-            places.keep_own(d);
-            float mean[1] = {lane_sum(d)};
-            lanes.sums(mean);
-            mean[0] /= static_cast<float>(dim);
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j) d[k][j] -= mean[0];
-            places.keep_own(d);
-            float both[2] = {lane_sum(d), lane_dot(d, d)};
-            lanes.sums(both);
-            return variance(both[0], both[1], dim, &c);
-        };
-        read();
+        for (int k = 0; k < NV; ++k) {
+            raw[k] = load_span(x, places.at[k], dim);
+            if (a.residual) more[k] = load_span(r0, places.at[k], dim);
+        }
+    };
+    const int64_t step = int64_t(gridDim.x) * kRows;
+    int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES;
+    if (kAhead && row < n) load(row);
+    for (; row < n; row += step) {
+        if (!kAhead) load(row);
         float s[NV][V];
-        if (a.sum) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int j = 0; j < V; ++j) s[k][j] = d[k][j];
-        }
-        float var = centre();
-        float mean = var + a.eps;
-        if (odd_row(var, a.eps, c)) {                      // (the same in all lanes of a row; nothing of the row is written yet, which may be in its input's place)
-            float s0 = static_cast<float>(x[0]);
-            if (a.residual) s0 += static_cast<float>(r0[0]);
-            const Unit u = odd_unit(mean);
-            read();
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j) d[k][j] = (d[k][j] * u.low - s0 * u.low) * u.high;
-            var = centre();
-            mean = unit_variance(var, a.eps, u.low * u.high);
-        }
-        const float r = 1.0f / sqrtf(mean);
+            for (int j = 0; j < V; ++j) {
+                s[k][j] = static_cast<float>(raw[k][j]);
+                if (a.residual) s[k][j] += static_cast<float>(more[k][j]);
+            }
+        if (kAhead && row + step < n) load(row + step);
         if (a.sum) {
             T *sum = static_cast<T *>(a.sum) + row * a.sum_stride;
 #pragma unroll
             for (int k = 0; k < NV; ++k) store_span<PAST>(sum, places.at[k], dim, s[k]);
         }
+        places.keep_own(s);
+        float centre, var;                                 // the mean but for its error, which is taken out of the variance here and of the values below
+        float c;
+        auto stats = [&]() __attribute__((always_inline)) {
+            float total[1] = {0.f};
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                float part = 0.f;
+#pragma unroll
+                for (int j = 0; j < V; ++j) part += s[k][j];
+                total[0] += part;
+            }
+            lanes.sums(total);
+            centre = mean_of(total[0], a.per_dim);
+            float both[2] = {0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                float part = 0.f, squares = 0.f;
+                places.for_own(k, [&](int j) __attribute__((always_inline)) {
+                    const float d = s[k][j] - centre;
+                    part += d;
+                    squares += d * d;
+                });
+                both[0] += part;
+                both[1] += squares;
+            }
+            lanes.sums(both);
+            var = variance(both[0], both[1], a.per_dim, &c);
+        };
+        stats();
+        float r;
+        if (!odd_row(var, a.eps, c)) {                     // (the same in all lanes of a row)
+            r = reciprocal_root(var + a.eps);
+        } else {
+            const Unit u = odd_unit(var + a.eps);
+            const float s0 = lanes.first(s[0][0]) * u.low;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) s[k][j] = (s[k][j] * u.low - s0) * u.high;
+            places.keep_own(s);
+            stats();
+            r = 1.0f / sqrtf(unit_variance(var, a.eps, u.low * u.high));
+        }
+        const float cr = c * r;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int j = 0; j < V; ++j) d[k][j] = fmaf((d[k][j] - c) * r, w[k][j], b[k][j]);
+            for (int j = 0; j < V; ++j) s[k][j] = fmaf(fmaf(s[k][j] - centre, r, -cr), w[k][j], b[k][j]);
         if (a.y) {
             T *y = static_cast<T *>(a.y) + row * a.y_stride;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) store_span<PAST>(y, places.at[k], dim, d[k]);
+            for (int k = 0; k < NV; ++k) store_span<PAST>(y, places.at[k], dim, s[k]);
         }
         if (!a.q) continue;
         uint8_t *q = a.q + row * a.q_stride;
         float *scale = a.scale + row * a.scale_stride;
-        places.keep_own(d);
+        places.keep_own(s);
         uint32_t most[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             most[k] = 0;
 #pragma unroll
-            for (int j = 0; j < V; ++j) most[k] = max_u32(most[k], __float_as_uint(d[k][j]) & 0x7FFFFFFFu);
+            for (int j = 0; j < V; ++j) most[k] = max_u32(most[k], __float_as_uint(s[k][j]) & 0x7FFFFFFFu);
         }
         if (group_lanes == 0) {
             uint32_t m = most[0];
@@ -273,7 +327,7 @@ k_layer_norm(LayerArgs a) {
             const Scale sc = scale_of(lanes.max(m), 1.f, top);
             if (lane == 0) scale[0] = sc.scale;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) store_q(q, places.at[k], dim, d[k], sc, a.q_type);
+            for (int k = 0; k < NV; ++k) store_q(q, places.at[k], dim, s[k], sc, a.q_type);
         } else {
             const int width = group_lanes < LANES ? group_lanes : LANES;
 #pragma unroll
@@ -281,7 +335,7 @@ k_layer_norm(LayerArgs a) {
                 const Scale sc = scale_of(lanes_max(most[k], width), 1.f, top);
                 const int i = k * LANES + lane;
                 if (lane % width == 0 && i * V < dim) scale[i / group_lanes] = sc.scale;
-                store_q(q, places.at[k], dim, d[k], sc, a.q_type);
+                store_q(q, places.at[k], dim, s[k], sc, a.q_type);
             }
         }
     }
@@ -295,7 +349,7 @@ struct LayerGradArgs {
     float *weight_parts, *bias_parts;      // every workgroup's share of the two gradients, `pitch` apart; null if not wanted
     int64_t gy_stride, s_stride, gs_stride, gx_stride, pitch;
     int64_t cap_rows;
-    float eps;
+    float eps, per_dim;
     int32_t dim;
 };
 
@@ -315,104 +369,135 @@ k_layer_norm_backward(LayerGradArgs a) {
     const int64_t n = rows_of(a.num_rows, a.cap_rows);
     const int dim = a.dim;
     const RowPlaces<LANES, NV, V> places(lane, dim);
-    float w[NV][V], gw[NV][V], gb[NV][V];
+    float w[NV][V];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        load_weight(a.weight, places.at[k], dim, w[k]);
-#pragma unroll
-        for (int j = 0; j < V; ++j) gw[k][j] = gb[k][j] = 0.f;
-    }
+    for (int k = 0; k < NV; ++k) load_weight(a.weight, places.at[k], dim, w[k]);
+    constexpr bool kInLds = kThreads >= 1024 && NV >= 2;   // (rows of 16,384: 4,000 of bf16 243 -> 166 us, 2,000 of fp32 207 -> 155; in LDS rows of 8,192 bf16 116 -> 137)
+    using Own = OwnSums<NV, V, kThreads, kInLds>;
+    __shared__ typename Own::Quad own[2 * Own::kQuads];
+    Own gw(own), gb(own + Own::kQuads);
     struct Row {
         W s[NV], g[NV], gs[NV];
     };
-    auto load = [&](int64_t row) __attribute__((always_inline)) {
-        Row v;
-        const T *sr = static_cast<const T *>(a.s) + row * a.s_stride;
-        const T *gr = static_cast<const T *>(a.grad_y) + row * a.gy_stride;
-        const T *gs = static_cast<const T *>(a.grad_sum) + row * a.gs_stride;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            v.s[k] = load_span(sr, places.at[k], dim);
-            v.g[k] = load_span(gr, places.at[k], dim);
-            if (a.grad_sum) v.gs[k] = load_span(gs, places.at[k], dim);
-        }
-        return v;
-    };
-    // A row is on its way while the one before is worked on, if the registers hold both.
-    constexpr bool kAhead = kThreads < 1024 || NV * V < 16;
     const int64_t step = int64_t(gridDim.x) * kRows;
     int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES;
-    Row next;
-    if (kAhead && row < n) next = load(row);
-    for (; row < n; row += step) {
-        const Row v = kAhead ? next : load(row);
-        if (kAhead && row + step < n) next = load(row + step);
-        places.keep_own(w);                                // (here a row's loads are on their way: before, they would wait for the weight's)
-        float d[NV][V], g[NV][V], h[NV][V];
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                d[k][j] = static_cast<float>(v.s[k][j]);
-                g[k][j] = static_cast<float>(v.g[k][j]);
-            }
-        places.keep_own(g);
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int j = 0; j < V; ++j) h[k][j] = g[k][j] * w[k][j];
-        float c = 0.f, dot = 0.f, h_mean = 0.f;
-        // d becomes its values less their mean, but for c; dot the mean of d h, h_mean that of h
-        auto centre = [&]() __attribute__((always_inline)) {
-            places.keep_own(d);
-            float first[2] = {lane_sum(d), lane_sum(h)};
-            lanes.sums(first);
-            first[0] /= static_cast<float>(dim);
-            h_mean = first[1] / static_cast<float>(dim);
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j) d[k][j] -= first[0];
-            places.keep_own(d);
-            float then[3] = {lane_sum(d), lane_dot(d, d), lane_dot(d, h)};
-            lanes.sums(then);
-            const float var = variance(then[0], then[1], dim, &c);
-            dot = then[2] / static_cast<float>(dim) - c * h_mean;
-            return var;
-        };
-        float var = centre(), unit = 1.f;
-        float mean = var + a.eps;
-        if (odd_row(var, a.eps, c)) {
-            const float s0 = static_cast<float>(*(static_cast<const T *>(a.s) + row * a.s_stride));
-            const Unit u = odd_unit(mean);
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j) d[k][j] = (static_cast<float>(v.s[k][j]) * u.low - s0 * u.low) * u.high;
-            unit = u.low * u.high;
-            var = centre();
-            mean = unit_variance(var, a.eps, unit);
-        }
-        const float r = 1.0f / sqrtf(mean);                // of d; the row's is r unit
-        dot *= r;
-        T *gx = static_cast<T *>(a.grad_x) + row * a.gx_stride;
+    const T *sr = static_cast<const T *>(a.s) + row * a.s_stride;
+    const T *gr = static_cast<const T *>(a.grad_y) + row * a.gy_stride;
+    const T *gs = static_cast<const T *>(a.grad_sum) + row * a.gs_stride;
+    T *gx = static_cast<T *>(a.grad_x) + row * a.gx_stride;
+    auto load = [&]() __attribute__((always_inline)) {
+        Row v;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            float out[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float u = (d[k][j] - c) * r;
-                gw[k][j] += g[k][j] * u;
-                gb[k][j] += g[k][j];
-                out[j] = r * unit * (h[k][j] - h_mean - u * dot);
-                if (a.grad_sum) out[j] += static_cast<float>(v.gs[k][j]);
-            }
-            store_span<PAST>(gx, places.at[k], dim, out);
+            v.s[k] = load_span<PAST>(sr, places.at[k], dim);
+            v.g[k] = load_span<PAST>(gr, places.at[k], dim);
+            if (a.grad_sum) v.gs[k] = load_span<PAST>(gs, places.at[k], dim);
         }
+        sr += step * a.s_stride;
+        gr += step * a.gy_stride;
+        gs += step * a.gs_stride;
+        return v;
+    };
+    constexpr bool kOpaque = kInLds;
+    // A row is on its way while the one before is worked on, if the registers hold both.
+    constexpr bool kAhead = kThreads < 1024 || NV * V < 16;
+    Row next;
+    if (kAhead && row < n) next = load();
+    for (; row < n; row += step) {
+        Row v = kAhead ? next : load();
+        if (kAhead && row + step < n) next = load();
+        places.keep_own(w);                                // (here a row's loads are on their way: before, they would wait for the weight's)
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (places.own[k] != places.kAll) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    v.s[k][j] = (places.own[k] >> j) & 1 ? v.s[k][j] : static_cast<T>(0.f);
+                    v.g[k][j] = (places.own[k] >> j) & 1 ? v.g[k][j] : static_cast<T>(0.f);
+                }
+            }
+        float centre, c, var, h_mean, dot;                 // the mean but for its error c; the mean of h, and of h with the differences from the mean
+        // Values are formed again where they are used: a row's registers hold it as it was loaded.  value(k, j): that of s
+        auto stats = [&](auto value) __attribute__((always_inline)) {
+            float before[2] = {0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                float p = 0.f, q = 0.f;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    p += value(k, j);
+                    q += static_cast<float>(v.g[k][j]) * w[k][j];
+                }
+                before[0] += p;
+                before[1] += q;
+            }
+            lanes.sums(before);
+            if (kOpaque) { as_loaded(v.s); as_loaded(v.g); }
+            centre = mean_of(before[0], a.per_dim);
+            h_mean = mean_of(before[1], a.per_dim);
+            float then[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                float p = 0.f, q = 0.f, t = 0.f;
+                places.for_own(k, [&](int j) __attribute__((always_inline)) {
+                    const float d = value(k, j) - centre;
+                    p += d;
+                    q += d * d;
+                    t += static_cast<float>(v.g[k][j]) * w[k][j] * d;
+                });
+                then[0] += p;
+                then[1] += q;
+                then[2] += t;
+            }
+            lanes.sums(then);
+            var = variance(then[0], then[1], a.per_dim, &c);
+            if (kOpaque) { as_loaded(v.s); as_loaded(v.g); }
+            dot = then[2] * a.per_dim - c * h_mean;
+        };
+        // r: of the values times `unit`
+        auto put_row = [&](auto value, float r, float unit) __attribute__((always_inline)) {
+            const float by = r * unit, cr = c * r;
+            dot *= r;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                float out[V], sum_w[V], sum_b[V];
+                gw.get(k, sum_w);
+                gb.get(k, sum_b);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float u = fmaf(value(k, j) - centre, r, -cr), g = static_cast<float>(v.g[k][j]);
+                    sum_w[j] = fmaf(g, u, sum_w[j]);
+                    sum_b[j] += g;
+                    out[j] = fmaf(-u, dot, g * w[k][j] - h_mean) * by;
+                    if (a.grad_sum) out[j] += static_cast<float>(v.gs[k][j]);
+                }
+                gw.put(k, sum_w);
+                gb.put(k, sum_b);
+                store_span<PAST>(gx, places.at[k], dim, out);
+            }
+        };
+        auto plain = [&](int k, int j) __attribute__((always_inline)) { return static_cast<float>(v.s[k][j]); };
+        stats(plain);
+        if (!odd_row(var, a.eps, c)) {
+            put_row(plain, reciprocal_root(var + a.eps), 1.f);
+        } else {
+            const Unit u = odd_unit(var + a.eps);
+            const float s0 = lanes.first(plain(0, 0)) * u.low;
+            auto scaled = [&](int k, int j) __attribute__((always_inline)) {
+                const float d = (static_cast<float>(v.s[k][j]) * u.low - s0) * u.high;
+                return (places.own[k] >> j) & 1 ? d : 0.f;
+            };
+            stats(scaled);
+            put_row(scaled, 1.0f / sqrtf(unit_variance(var, a.eps, u.low * u.high)), u.low * u.high);
+        }
+        gx += step * a.gx_stride;
     }
     // The workgroup's share of a gradient.
-    auto put = [&](float *parts, float (&v)[NV][V]) __attribute__((always_inline)) {
+    auto put = [&](float *parts, const Own &sums) __attribute__((always_inline)) {
         if (!parts) return;
+        float v[NV][V];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) sums.get(k, v[k]);
         float *part = parts + int64_t(blockIdx.x) * a.pitch;
         if constexpr (LANES > kWave) {                     // the workgroup is one row's: nothing to join
 #pragma unroll
@@ -451,7 +536,11 @@ int launch_layer_norm(mqg_ctx *ctx, const LayerArgs &a, hipStream_t s) {
     const int64_t cells = a.cap_rows * a.dim, arrays = 1 + (a.residual != nullptr) + (a.sum != nullptr) + (a.y != nullptr);
     const bool past = cells * (arrays * int64_t(sizeof(T)) + (a.q != nullptr)) >= kPastBytes;
     const int threads = std::max(sh.lanes, kBlock);
-    const int64_t most = sizeof(T) == 4 ? (int64_t(1) << 31) - 1 : int64_t(8192) * kBlock / threads;
+    // Several sets of rows to a workgroup, which reads weight and bias once: 109,000 x 602 fp32 with 2,048, 4,096, 16,384 workgroups of 256 threads 207, 204 and 190 us,
+    // without a limit 201; 300,000 x 100 101, 95, 87 and 97; 295,000 x 256 fp16 into e4m3 with 2,048, 4,096 and 8,192 111, 108 and 101.  The longest fp32 rows, of which no second
+    // one is on its way, 4,000 x 16,384: 186 with 1,024 of 1,024 threads, 214 with one a row.
+    const bool longest = threads == 1024 && sh.nv > 2;
+    const int64_t most = int64_t(sizeof(T) == 4 && !longest ? 16384 : longest ? 4096 : 8192) * kBlock / threads;
     const int64_t grid = std::min<int64_t>(std::min<int64_t>(ceil_div(a.cap_rows, threads / sh.lanes), most), ((int64_t(1) << 32) - 1) / threads);
 #define MQG_GO(T, L, N)                                                                                                            \
     do {                                                                                                                           \
@@ -463,15 +552,26 @@ int launch_layer_norm(mqg_ctx *ctx, const LayerArgs &a, hipStream_t s) {
     return MQG_OK;
 }
 
+// How a backward's rows are laid out: those of 16 bits that would take three or four vectors of a wavefront's lanes have four wavefronts (registers for one row on its way
+// beside the sums: 20,000 x 2,000 bf16 90 -> 72 us; 30,000 x 1,500 90 -> 86).
+RowShape grad_shape(int dim, int vec, int64_t rows) {
+    const RowShape sh = row_shape(dim, vec, rows);
+    return sh.lanes == kWave && sh.nv * vec > 16 ? RowShape{256, 1} : sh;
+}
+// Workgroups of a backward at most, each of which leaves its share of the gradients: as many as are on the chip together for the longest rows (8,192 x 8,192
+// bf16: 256 103 us, 512 116), more for short ones (2 M x 16 bf16: 512 79, 1,024 63) and for those of four wavefronts (20,000 x 2,000: 80 and 73); in between
+// 295,000 x 256 fp16 512 98, 1,024 105; 109,000 x 602 fp32 176 and 184.
+int grad_parts(const RowShape &sh) { return sh.lanes <= 16 || sh.lanes == 256 ? 1024 : sh.lanes * sh.nv >= 1024 ? 256 : 512; }
+
 template <typename T>
 int launch_layer_norm_backward(mqg_ctx *ctx, LayerGradArgs a, float *grad_weight, float *grad_bias, hipStream_t s) {
-    const RowShape sh = row_shape(a.dim, Vec<T>::kLen, a.cap_rows);
+    const RowShape sh = grad_shape(a.dim, Vec<T>::kLen, a.cap_rows);
     const int threads = std::max(sh.lanes, kBlock);
     const int64_t sets = ceil_div(a.cap_rows, threads / sh.lanes);
     const int wanted = (grad_weight != nullptr) + (grad_bias != nullptr);
     // Rows of a few rounds are one workgroup's, whose sums are the gradients, and the second launch falls away.
     const bool alone = wanted && sets > 0 && sets <= (sh.lanes <= kBlock ? 4 : 2);
-    const int grid = alone ? 1 : static_cast<int>(std::min<int64_t>(sets, kNormParts));
+    const int grid = alone ? 1 : static_cast<int>(std::min<int64_t>(sets, grad_parts(sh)));
     const bool past = a.cap_rows * a.dim * (a.grad_sum ? 4 : 3) * int64_t(sizeof(T)) >= kPastBytes;
     a.pitch = int64_t(wanted) * a.dim;
     float *parts = nullptr;
@@ -510,7 +610,7 @@ int run_layer_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *re
                    int64_t y_stride, void *q, int64_t q_stride, int32_t q_type, int32_t group, float *scale, int64_t scale_stride, hipStream_t s) {
     if (cap_rows == 0) return MQG_OK;
     const LayerArgs a{x, residual, weight, bias, num_rows, sum, y, static_cast<uint8_t *>(q), scale, x_stride, residual_stride, sum_stride,
-                      y_stride, q_stride, scale_stride, cap_rows, eps, dim, q_type, group};
+                      y_stride, q_stride, scale_stride, cap_rows, eps, 1.0f / static_cast<float>(dim), dim, q_type, group};
     if (dtype == MQG_F16) return launch_layer_norm<F16>(ctx, a, s);
     if (dtype == MQG_BF16) return launch_layer_norm<BF16>(ctx, a, s);
     return launch_layer_norm<float>(ctx, a, s);
@@ -520,7 +620,7 @@ int run_layer_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride,
                             const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows, int64_t cap_rows, int32_t dim,
                             int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, float *grad_bias, hipStream_t s) {
     const LayerGradArgs a{grad_y, sum, grad_sum, weight, num_rows, grad_x, nullptr, nullptr, gy_stride, sum_stride, gs_stride, gx_stride, 0, cap_rows,
-                          eps, dim};
+                          eps, 1.0f / static_cast<float>(dim), dim};
     if (dtype == MQG_F16) return launch_layer_norm_backward<F16>(ctx, a, grad_weight, grad_bias, s);
     if (dtype == MQG_BF16) return launch_layer_norm_backward<BF16>(ctx, a, grad_weight, grad_bias, s);
     return launch_layer_norm_backward<float>(ctx, a, grad_weight, grad_bias, s);

@@ -64,12 +64,13 @@ struct Span {
     __device__ __forceinline__ bool mine(int j) const { return j >= skip; }
 };
 // Its elements as they lie; nothing outside the row is read, zeros past the end of a row of fewer than V.
-template <typename T>
+template <bool PAST = false, typename T>
 __device__ __forceinline__ typename Vec<T>::Whole load_span(const T *row, const Span<Vec<T>::kLen> &at, int dim) {
     constexpr int V = Vec<T>::kLen;
     typename Vec<T>::Whole v;
     if (dim >= V) {
-        v = *reinterpret_cast<const typename Vec<T>::Any *>(row + at.base);
+        if constexpr (PAST) v = __builtin_nontemporal_load(reinterpret_cast<const typename Vec<T>::Any *>(row + at.base));
+        else v = *reinterpret_cast<const typename Vec<T>::Any *>(row + at.base);
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = j < dim ? row[j] : static_cast<T>(0.f);
