@@ -806,8 +806,8 @@ typedef struct mqg_adamw {
  *   n = mul * sqrt(sum over all gradients of g^2),   scale = mul * min(1, max_norm / n)
  * mul: what the gradients are to be multiplied by in any case (1, or one over a loss scale); max_norm: INFINITY = no limit.
  * norm, scale: device float, either may be NULL.  A norm that is not finite in fp32 gives the scale NaN, with which mqg_adamw_step steps nothing.
- * Squares are added in fp32 sixteen at a time and in double above, whatever the gradients' size, in an order that depends on the list's sizes and
- * types alone: the same bits in every call.  Nothing is allocated.
+ * Squares are added in fp32 sixteen at a time and in double above, whatever the gradients' size, in an order that depends on the list's sizes, types
+ * and addresses (their places in lines of 128 bytes) alone: the same bits in every call.  Nothing is allocated.
  */
 int mqg_grad_norm(mqg_ctx *ctx, const mqg_param *params, int32_t num_params, float mul, float max_norm, float *norm, float *scale,
                   mqg_stream stream);
@@ -816,7 +816,7 @@ int mqg_grad_norm(mqg_ctx *ctx, const mqg_param *params, int32_t num_params, flo
  * An AdamW step of every tensor of a list, with g = grad_scale * grad:
  *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2
  *   weight <- (1 - lr weight_decay) weight - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
- * in fp32 (no change where the divisor is zero), each result rounded once, to nearest even.  Weights of 16 bits are rounded at every step, which loses steps of
+ * in fp32 (no change where the divisor is zero; an eps below 2^-126 counts as zero), each result rounded once, to nearest even.  Weights of 16 bits are rounded at every step, which loses steps of
  * less than half their last place: keep those in MQG_F32 and take a copy of 16 bits.
  *   MQG_STATE_E4M3   m = m_scale * value and sqrt(v) = v_scale * value, e4m3 values with a scale per MQG_ADAMW_BLOCK elements in order (the last block may be
  *              shorter), scale = max(max |.| / 448, 2^-126), values rounded to nearest, ties to even, a root above zero to 2^-9 at least.  The step itself

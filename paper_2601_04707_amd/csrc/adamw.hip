@@ -96,10 +96,9 @@ struct StepArgs {
     uint32_t rest[kTensors];             // the last workgroup's elements less one, factors << 16, shift << 24 (of moments in 32 bits: blocks of 8-bit ones are counted from the tensor's beginning)
     void set(int which, int tensor, const void *p) {
         const uint64_t at = reinterpret_cast<uint64_t>(p);
-        const int by = which % 2 * 16;
-        uint32_t &h = high[which / 2][tensor];
+        const uint32_t half = static_cast<uint32_t>(at >> 32 & 0xFFFF);
         low[which][tensor] = static_cast<uint32_t>(at);
-        h = (h & ~(0xFFFFu << by)) | static_cast<uint32_t>(at >> 32 & 0xFFFF) << by;
+        high[which / 2][tensor] = which % 2 == 0 ? half : high[which / 2][tensor] | half << 16;       // (in order)
     }
     __device__ __forceinline__ void *get(int which, int tensor) const {
         const uint64_t at = static_cast<uint64_t>(high[which / 2][tensor] >> which % 2 * 16 & 0xFFFF) << 32 | low[which][tensor];
@@ -628,7 +627,7 @@ int run_adamw_step(mqg_ctx *ctx, const mqg_param *params, int32_t num, const mqg
     a.step = plan->step_dev;
     a.lr_dev = plan->lr_dev;
     a.grad_scale = plan->grad_scale_dev;
-    a.eps = static_cast<float>(plan->eps);
+    a.eps = plan->eps < 0x1p-126 ? 0.f : static_cast<float>(plan->eps);
     // Tensors of the same types go together.  A kind: the types of weight and gradient, that of the moments, and that of the copy (3: none).
     auto kind_of = [](const mqg_param &p) { return ((p.weight_type * 3 + p.grad_type) * 2 + p.state_type) * 4 + (p.copy ? p.copy_type : 3); };
     constexpr int kKinds = 3 * 3 * 2 * 4;

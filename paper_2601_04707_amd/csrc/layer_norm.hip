@@ -563,6 +563,31 @@ RowShape grad_shape(int dim, int vec, int64_t rows) {
 // 295,000 x 256 fp16 512 98, 1,024 105; 109,000 x 602 fp32 176 and 184.
 int grad_parts(const RowShape &sh) { return sh.lanes <= 16 || sh.lanes == 256 ? 1024 : sh.lanes * sh.nv >= 1024 ? 256 : 512; }
 
+#define MQG_GRAD_SHAPES(T, GO)                                     \
+    switch (sh.lanes) {                                            \
+        case 4: GO(T, 4, 1); break;                                \
+        case 8: GO(T, 8, 1); break;                                \
+        case 16: GO(T, 16, 1); break;                              \
+        case 32: GO(T, 32, 1); break;                              \
+        case 64:                                                   \
+            if (sh.nv == 1) GO(T, 64, 1);                          \
+            else if (sh.nv == 2) GO(T, 64, 2);                     \
+            else if constexpr (sizeof(T) == 4) {                   \
+                if (sh.nv == 3) GO(T, 64, 3);                      \
+                else GO(T, 64, 4);                                 \
+            }                                                      \
+            break;                                                 \
+        case 256: GO(T, 256, 1); break;                            \
+        case 512:                                                  \
+            if (sh.nv == 1) GO(T, 512, 1);                         \
+            else GO(T, 512, 2);                                    \
+            break;                                                 \
+        default:                                                   \
+            if (sh.nv == 1) GO(T, 1024, 1);                        \
+            else if (sh.nv == 2) GO(T, 1024, 2);                   \
+            else if constexpr (sizeof(T) == 4) GO(T, 1024, 4);     \
+    }
+
 template <typename T>
 int launch_layer_norm_backward(mqg_ctx *ctx, LayerGradArgs a, float *grad_weight, float *grad_bias, hipStream_t s) {
     const RowShape sh = grad_shape(a.dim, Vec<T>::kLen, a.cap_rows);
@@ -591,7 +616,7 @@ int launch_layer_norm_backward(mqg_ctx *ctx, LayerGradArgs a, float *grad_weight
         else MQG_LAUNCH(ctx, "k_layer_norm_backward", s, (k_layer_norm_backward<T, L, N, false><<<grid, threads, 0, s>>>(a)));                \
     } while (0)
     if (grid > 0) {
-        MQG_NORM_SHAPES(T, MQG_GO)
+        MQG_GRAD_SHAPES(T, MQG_GO)
     }
 #undef MQG_GO
     if (wanted && !alone) {

@@ -242,14 +242,15 @@ def test_steps_in_a_row_from_nothing(mqg, ctx, bits):
 
 def test_no_step_where_nothing_is_known_and_without_an_epsilon(mqg, ctx):
     for bits in (32, 8):
-        c = Case(300, torch.Generator().manual_seed(4), bits=bits, fresh=True)
-        c.grad.t[::3] = 0
-        plan = dict(PLAN, eps=0.0, step=1)
-        expect([c], plan)
-        mqg.mqg_adamw_step(ctx, params_of(mqg, [c]), **plan)
-        torch.cuda.synchronize()
-        assert bool(c.weight.t.isfinite().all())
-        c.check()
+        for eps in (0.0, 1e-42):                                         # the second one is below fp32's normal numbers
+            c = Case(300, torch.Generator().manual_seed(4), bits=bits, fresh=True)
+            c.grad.t[::3] = 0
+            plan = dict(PLAN, eps=eps, step=1)
+            expect([c], dict(plan, eps=0.0))
+            mqg.mqg_adamw_step(ctx, params_of(mqg, [c]), **plan)
+            torch.cuda.synchronize()
+            assert bool(c.weight.t.isfinite().all())
+            c.check()
 
 
 def test_a_block_of_zeros_and_the_smallest_roots_in_8_bits(mqg, ctx):
