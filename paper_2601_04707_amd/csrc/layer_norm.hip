@@ -159,6 +159,34 @@ __device__ __forceinline__ void as_loaded(W (&v)[NV]) {
     for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(v[k]));
 }
 
+// How a group is taken to 8 bits: by max|y| / top as it is before it is rounded to the scale, in two terms, so that one rounding of those that can bring a value to the other side of a
+// border falls away.  most and NaN as of the other norm.
+struct FineScale {
+    float scale, lo, inv;
+};
+__device__ __forceinline__ FineScale fine_scale(uint32_t most, float top) {
+    const float m = __uint_as_float(most), per_top = 1.0f / top, t = m / top;
+    if (!(t < __uint_as_float(0x7F800000u))) {
+        const float nan = __uint_as_float(0x7FC00000u);
+        return {nan, nan, nan};
+    }
+    if (!(t > 0x1p-100f)) {                                // (its second term would be below 32 bits' numbers)
+        const float least = fmaxf(t, 0x1p-126f);
+        return {least, 0.f, 1.0f / least};
+    }
+    return {t, fmaf(-t, top, m) * per_top, 1.0f / t};
+}
+template <int V>
+__device__ __forceinline__ void to_8bit(const float (&z)[V], const FineScale &s, int q_type, uint32_t (&w)[V / 4]) {
+    float y[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const float quot = z[j] * s.inv;
+        y[j] = fmaf(fmaf(-quot, s.lo, fmaf(-quot, s.scale, z[j])), s.inv, quot);
+    }
+    pack_8bit(y, s.scale == s.scale, q_type, w);
+}
+
 template <int V>
 __device__ __forceinline__ void load_bias(const float *b, const Span<V> &at, int dim, float (&out)[V]) {
     if (b) {
@@ -269,6 +297,8 @@ k_layer_norm(LayerArgs a) {
             }
             lanes.sums(total);
             centre = mean_of(total[0], a.per_dim);
+            // Of 16-bit rows a mean of 12 bits, from which the differences are exact; the rest of it is theirs, c.
+            if (sizeof(T) == 2) centre = __uint_as_float(__float_as_uint(centre) & 0xFFFFF000u);
             float both[2] = {0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
@@ -324,7 +354,7 @@ k_layer_norm(LayerArgs a) {
             uint32_t m = most[0];
 #pragma unroll
             for (int k = 1; k < NV; ++k) m = max_u32(m, most[k]);
-            const Scale sc = scale_of(lanes.max(m), 1.f, top);
+            const FineScale sc = fine_scale(lanes.max(m), top);
             if (lane == 0) scale[0] = sc.scale;
 #pragma unroll
             for (int k = 0; k < NV; ++k) store_q(q, places.at[k], dim, s[k], sc, a.q_type);
@@ -332,7 +362,7 @@ k_layer_norm(LayerArgs a) {
             const int width = group_lanes < LANES ? group_lanes : LANES;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                const Scale sc = scale_of(lanes_max(most[k], width), 1.f, top);
+                const FineScale sc = fine_scale(lanes_max(most[k], width), top);
                 const int i = k * LANES + lane;
                 if (lane % width == 0 && i * V < dim) scale[i / group_lanes] = sc.scale;
                 store_q(q, places.at[k], dim, s[k], sc, a.q_type);

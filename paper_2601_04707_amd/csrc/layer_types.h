@@ -185,16 +185,9 @@ __device__ __forceinline__ Scale scale_of(uint32_t most, float r, float top) {
     return t > 0x1p-100f ? Scale{scale, 1.f, t} : Scale{scale, r, scale};
 }
 
-// V values in 8 bits, four to a word.
+// V quotients in 8 bits, four to a word.  number: their scale is one
 template <int V>
-__device__ __forceinline__ void to_8bit(const float (&z)[V], const Scale &s, int q_type, uint32_t (&w)[V / 4]) {
-    const float inv = 1.0f / s.div;
-    float y[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {                          // the quotient by the reciprocal, and its remainder's
-        const float num = z[j] * s.by, quot = num * inv;
-        y[j] = fmaf(fmaf(-quot, s.div, num), inv, quot);
-    }
+__device__ __forceinline__ void pack_8bit(const float (&y)[V], bool number, int q_type, uint32_t (&w)[V / 4]) {
     if (q_type == MQG_Q_E4M3) {
 #pragma unroll
         for (int k = 0; k < V / 4; ++k) {
@@ -202,7 +195,6 @@ __device__ __forceinline__ void to_8bit(const float (&z)[V], const Scale &s, int
             w[k] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2], y[4 * k + 3], p, true));
         }
     } else {
-        const bool number = s.scale == s.scale;
 #pragma unroll
         for (int k = 0; k < V / 4; ++k) {
             w[k] = 0;
@@ -213,6 +205,18 @@ __device__ __forceinline__ void to_8bit(const float (&z)[V], const Scale &s, int
             }
         }
     }
+}
+// V values in 8 bits
+template <int V>
+__device__ __forceinline__ void to_8bit(const float (&z)[V], const Scale &s, int q_type, uint32_t (&w)[V / 4]) {
+    const float inv = 1.0f / s.div;
+    float y[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {                          // the quotient by the reciprocal, and its remainder's
+        const float num = z[j] * s.by, quot = num * inv;
+        y[j] = fmaf(fmaf(-quot, s.div, num), inv, quot);
+    }
+    pack_8bit(y, s.scale == s.scale, q_type, w);
 }
 
 }  // namespace mqg

@@ -37,8 +37,8 @@ __device__ __forceinline__ float of_wave(float v) {
 }
 
 // V values of a row in 8 bits
-template <int V>
-__device__ __forceinline__ void store_q(uint8_t *row, const Span<V> &at, int dim, const float (&z)[V], const Scale &s, int q_type) {
+template <int V, typename S>
+__device__ __forceinline__ void store_q(uint8_t *row, const Span<V> &at, int dim, const float (&z)[V], const S &s, int q_type) {
     uint32_t w[V / 4];
     to_8bit(z, s, q_type, w);
     if (at.skip == 0 && dim >= V) {
