@@ -19,8 +19,10 @@
 namespace mqg {
 namespace {
 
-// A call that moves twice what the chip's memory-side cache holds goes past the caches, with its loads, too.
-constexpr int64_t kPastBytes = int64_t(512) << 20;
+// Steps that move more than half of what the chip's memory-side cache holds go past the caches, with their loads, too: what lies between two steps of a program leaves nothing
+// there (on buffers in turn: 12.8 M elements in 32 bits, 358 MB, 81 -> 69 us; with 8-bit moments and bf16 copies, 206 MB, 50 -> 46; 100 M, 2.8 GB, 517 -> 463.  3.2 M, 91 MB,
+// 16.2 -> 19.3).  The norm's reads do where the gradients don't fit: the step reads those again (202 MB of them: norm and step 474, past the caches 504).
+constexpr int64_t kStepPastBytes = int64_t(128) << 20, kNormPastBytes = int64_t(256) << 20;
 constexpr int64_t kMostElems = int64_t(1) << 31;       // of a launch; longer tensors go in parts
 
 // x + y of two products, each rounded by itself: 8-bit moments go from step to step, where one that falls to the other side of a rounding border is a sixteenth
@@ -570,7 +572,7 @@ int run_grad_norm(mqg_ctx *ctx, const mqg_param *params, int32_t num, float mul,
         }
         types += met;
     }
-    const bool join = types == 1 && wanted <= kNormTensors && all_chunks <= kJoinParts, past = bytes >= kPastBytes;
+    const bool join = types == 1 && wanted <= kNormTensors && all_chunks <= kJoinParts, past = bytes >= kNormPastBytes;
     int parts = 0;
     for (int32_t type : {MQG_F32, MQG_F16, MQG_BF16}) {
         a.count = 0;
@@ -646,7 +648,7 @@ int run_adamw_step(mqg_ctx *ctx, const mqg_param *params, int32_t num, const mqg
         met[kind_of(p)] = true;
         bytes += p.numel * (2 * type_size(p.weight_type) + type_size(p.grad_type) + (p.copy ? type_size(p.copy_type) : 0) + (p.state_type == MQG_STATE_E4M3 ? 4 : 16));
     }
-    const bool past = bytes >= kPastBytes;
+    const bool past = bytes >= kStepPastBytes;
     for (int kind = 0; kind < kKinds; ++kind) {
         if (!met[kind]) continue;
         auto wanted = [&](const mqg_param &p) { return p.grad && p.numel > 0 && kind_of(p) == kind; };

@@ -119,7 +119,8 @@ struct mqg_ctx {
     int64_t cache_arena_bytes = 0;
     // what the calls of a layer leave between their launches (norm.hip, orthogonal.hip); grows with the calls, or by mqg_ctx_reserve_layer
     mqg::Arena layer_scratch;
-    double *norm_parts = nullptr;        // [kGradNormParts + 1] sums of squares of the workgroups of a gradients' norm, and how many have theirs (adamw.hip)
+    double *norm_parts = nullptr;        // [kGradNormParts + 1] sums of squares of the workgroups of a gradients' norm, and how many have theirs (adamw.hip); how many
+                                         // workgroups of a layer norm's backward have theirs (layer_norm.hip)
     // hash-table dedup (MQG_OPT_DEDUP_HASH); allocated when the option is first used
     bool dedup_hash = false;
     unsigned long long *hash_table = nullptr;      // [hash_capacity] (id << 32 | position), all ones = empty

@@ -17,6 +17,11 @@ int64_t layer_norm_scratch_bytes(int32_t dim) { return std::max(std::min<int64_t
 
 namespace {
 
+// A call that moves more than the chip's memory-side cache holds goes past the caches, with its loads, too (buffers that it doesn't hold from the call before: 295,000 x 256 fp16
+// into e4m3 98 -> 85 us, 109,000 x 602 fp32 197 with all through the caches, 188 with the stores past them, 175; its backward 204, 195, 176; 1 M x 64 bf16 94 -> 87; 40,000 x 1,000 bf16
+// 57 either way).  Smaller ones leave their output there for the next reader.
+constexpr int64_t kLayerPastBytes = int64_t(256) << 20;
+
 struct LayerArgs {
     const void *x, *residual;
     const float *weight, *bias;
@@ -260,8 +265,8 @@ k_layer_norm(LayerArgs a) {
         const T *r0 = static_cast<const T *>(a.residual) + row * a.residual_stride;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            raw[k] = load_span(x, places.at[k], dim);
-            if (a.residual) more[k] = load_span(r0, places.at[k], dim);
+            raw[k] = load_span<PAST>(x, places.at[k], dim);
+            if (a.residual) more[k] = load_span<PAST>(r0, places.at[k], dim);
         }
     };
     const int64_t step = int64_t(gridDim.x) * kRows;
@@ -377,6 +382,9 @@ struct LayerGradArgs {
     const int64_t *num_rows;
     void *grad_x;
     float *weight_parts, *bias_parts;      // every workgroup's share of the two gradients, `pitch` apart; null if not wanted
+    uint32_t *done;                        // few columns and workgroups: those that have left their shares, of which the last adds them all; else null
+    float *sum, *sum_bias;                 // ... to the gradients (`split` columns of the first)
+    int32_t split;
     int64_t gy_stride, s_stride, gs_stride, gx_stride, pitch;
     int64_t cap_rows;
     float eps, per_dim;
@@ -558,13 +566,43 @@ k_layer_norm_backward(LayerGradArgs a) {
     };
     put(a.weight_parts, gw);
     put(a.bias_parts, gb);
+    if constexpr (LANES <= kWave) {
+        if (!a.done) return;
+        __shared__ bool last;
+        __shared__ float joined[kThreads];
+        const int tid = static_cast<int>(threadIdx.x), cols = static_cast<int>(a.pitch), num = static_cast<int>(gridDim.x);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent"); // (every wavefront's share, past its die's L2)
+        __syncthreads();
+        if (tid == 0) last = __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x;
+        __syncthreads();
+        if (!last) return;
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+        if (tid == 0) __hip_atomic_store(a.done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        // as many threads to a column as there are, each of which takes shares in turn; their sums in order
+        const float *parts = a.weight_parts ? a.weight_parts : a.bias_parts;
+        const int turns = kThreads / (2 * a.split), turn = tid / cols, col = tid % cols;     // (the same whether one gradient is wanted or both)
+        constexpr int kOnTheWay = 16;
+        float x = 0.f;
+        for (int p0 = turn; turn < turns && p0 < num; p0 += kOnTheWay * turns) {
+            float y[kOnTheWay];
+#pragma unroll
+            for (int k = 0; k < kOnTheWay; ++k) y[k] = p0 + k * turns < num ? parts[(p0 + k * turns) * cols + col] : 0.f;
+#pragma unroll
+            for (int k = 0; k < kOnTheWay; ++k) x += y[k];
+        }
+        joined[tid] = x;
+        __syncthreads();
+        if (tid >= cols) return;
+        for (int k = 1; k < turns; ++k) x += joined[k * cols + tid];
+        *(tid < a.split ? a.sum + tid : a.sum_bias + (tid - a.split)) = x;
+    }
 }
 
 template <typename T>
 int launch_layer_norm(mqg_ctx *ctx, const LayerArgs &a, hipStream_t s) {
     const RowShape sh = row_shape(a.dim, Vec<T>::kLen, a.cap_rows);
     const int64_t cells = a.cap_rows * a.dim, arrays = 1 + (a.residual != nullptr) + (a.sum != nullptr) + (a.y != nullptr);
-    const bool past = cells * (arrays * int64_t(sizeof(T)) + (a.q != nullptr)) >= kPastBytes;
+    const bool past = cells * (arrays * int64_t(sizeof(T)) + (a.q != nullptr)) >= kLayerPastBytes;
     const int threads = std::max(sh.lanes, kBlock);
     // Several sets of rows to a workgroup, which reads weight and bias once: 109,000 x 602 fp32 with 2,048, 4,096, 16,384 workgroups of 256 threads 207, 204 and 190 us,
     // without a limit 201; 300,000 x 100 101, 95, 87 and 97; 295,000 x 256 fp16 into e4m3 with 2,048, 4,096 and 8,192 111, 108 and 101.  The longest fp32 rows, of which no second
@@ -592,6 +630,8 @@ RowShape grad_shape(int dim, int vec, int64_t rows) {
 // bf16: 256 103 us, 512 116), more for short ones (2 M x 16 bf16: 512 79, 1,024 63) and for those of four wavefronts (20,000 x 2,000: 80 and 73); in between
 // 295,000 x 256 fp16 512 98, 1,024 105; 109,000 x 602 fp32 176 and 184.
 int grad_parts(const RowShape &sh) { return sh.lanes <= 16 || sh.lanes == 256 ? 1024 : sh.lanes * sh.nv >= 1024 ? 256 : 512; }
+
+constexpr int kJoinGrid = 32;         // workgroups whose shares the last of them adds
 
 #define MQG_GRAD_SHAPES(T, GO)                                     \
     switch (sh.lanes) {                                            \
@@ -627,7 +667,7 @@ int launch_layer_norm_backward(mqg_ctx *ctx, LayerGradArgs a, float *grad_weight
     // Rows of a few rounds are one workgroup's, whose sums are the gradients, and the second launch falls away.
     const bool alone = wanted && sets > 0 && sets <= (sh.lanes <= kBlock ? 4 : 2);
     const int grid = alone ? 1 : static_cast<int>(std::min<int64_t>(sets, grad_parts(sh)));
-    const bool past = a.cap_rows * a.dim * (a.grad_sum ? 4 : 3) * int64_t(sizeof(T)) >= kPastBytes;
+    const bool past = a.cap_rows * a.dim * (a.grad_sum ? 4 : 3) * int64_t(sizeof(T)) >= kLayerPastBytes;
     a.pitch = int64_t(wanted) * a.dim;
     float *parts = nullptr;
     if (alone) {
@@ -640,6 +680,16 @@ int launch_layer_norm_backward(mqg_ctx *ctx, LayerGradArgs a, float *grad_weight
         a.weight_parts = grad_weight ? parts : nullptr;
         a.bias_parts = grad_bias ? parts + (grad_weight ? a.dim : 0) : nullptr;
     }
+    // The join of few shares of few columns in the last workgroup saves a launch, but every workgroup waits until its share is past its die: 300 x 64 bf16, 19 workgroups, 7.7 us a call
+    // against 10.9, 1,400 x 64 fp32, 88, 10.8 either way, 1,000 x 128, 125, 16.1 against 10.9.
+    const int cols = wanted * a.dim;
+    const bool join = parts && grid > 0 && grid <= kJoinGrid && 2 * a.dim <= kBlock && threads == kBlock;
+    if (join) {
+        a.done = reinterpret_cast<uint32_t *>(ctx->norm_parts + kGradNormParts) + 1;
+        a.sum = grad_weight ? grad_weight : grad_bias;
+        a.sum_bias = grad_bias;
+        a.split = a.dim;
+    }
 #define MQG_GO(T, L, N)                                                                                                                  \
     do {                                                                                                                                 \
         if (past) MQG_LAUNCH(ctx, "k_layer_norm_backward", s, (k_layer_norm_backward<T, L, N, true><<<grid, threads, 0, s>>>(a)));            \
@@ -649,8 +699,7 @@ int launch_layer_norm_backward(mqg_ctx *ctx, LayerGradArgs a, float *grad_weight
         MQG_GRAD_SHAPES(T, MQG_GO)
     }
 #undef MQG_GO
-    if (wanted && !alone) {
-        const int cols = wanted * a.dim;
+    if (parts && !join) {
         MQG_LAUNCH(ctx, "k_sum_parts", s,
                    (k_sum_parts<<<static_cast<int>(ceil_div(cols, kSumCols)), kSumThreads, 0, s>>>(parts, grid, cols, grad_weight ? grad_weight : grad_bias,
                                                                                                     a.dim, grad_bias)));
@@ -674,7 +723,7 @@ int run_layer_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *re
 int run_layer_norm_backward(mqg_ctx *ctx, const void *grad_y, int64_t gy_stride, const void *sum, int64_t sum_stride, const float *weight,
                             const void *grad_sum, int64_t gs_stride, float eps, const int64_t *num_rows, int64_t cap_rows, int32_t dim,
                             int32_t dtype, void *grad_x, int64_t gx_stride, float *grad_weight, float *grad_bias, hipStream_t s) {
-    const LayerGradArgs a{grad_y, sum, grad_sum, weight, num_rows, grad_x, nullptr, nullptr, gy_stride, sum_stride, gs_stride, gx_stride, 0, cap_rows,
+    const LayerGradArgs a{grad_y, sum, grad_sum, weight, num_rows, grad_x, nullptr, nullptr, nullptr, nullptr, nullptr, 0, gy_stride, sum_stride, gs_stride, gx_stride, 0, cap_rows,
                           eps, 1.0f / static_cast<float>(dim), dim};
     if (dtype == MQG_F16) return launch_layer_norm_backward<F16>(ctx, a, grad_weight, grad_bias, s);
     if (dtype == MQG_BF16) return launch_layer_norm_backward<BF16>(ctx, a, grad_weight, grad_bias, s);

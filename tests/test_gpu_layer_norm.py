@@ -369,6 +369,26 @@ def test_backward_of_a_few_rows(mqg, ctx, dim, dtype):
             assert bool((gx[valid:] == MARK).all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_backward_of_few_columns_call_after_call(mqg, ctx, dtype):
+    """Shares that the last workgroup adds: any number of workgroups, the same bits in every call, and what the device counts in between."""
+    gen = torch.Generator().manual_seed(14)
+    for dim, rows in ((1, 300), (3, 9000), (64, 1400), (64, 2048), (100, 700), (128, 1100), (128, 5000), (129, 1100)):
+        s, gy = (torch.randn((rows, dim), generator=gen).to(dtype).cuda() for _ in range(2))
+        w = (1 + 0.3 * torch.randn(dim, generator=gen)).cuda()
+        first = None
+        for call in range(6):
+            count = rows if call != 3 else rows // 3
+            gx, gw, gb = torch.zeros_like(s), torch.full((dim,), MARK, device="cuda"), torch.full((dim,), MARK, device="cuda")
+            mqg.mqg_layer_norm_backward(ctx, gy, s, w, gx, grad_weight=gw, grad_bias=gb, eps=EPS, num_rows=torch.tensor([count], device="cuda"))
+            torch.cuda.synchronize()
+            if call in (0, 3):
+                check_backward(gx[:count], gw, gb, backward64(gy[:count], s[:count], w, None), dtype, rows)
+                first = (gw, gb) if call == 0 else first
+            else:
+                assert torch.equal(gw, first[0]) and torch.equal(gb, first[1]), (dim, rows, call)
+
+
 @pytest.mark.parametrize("bad", [float("inf"), float("nan")])
 def test_a_weight_that_is_not_finite_stays_its_own_columns(mqg, ctx, bad):
     for dim in (10, 250, 3000):
