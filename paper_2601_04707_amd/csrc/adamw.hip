@@ -7,8 +7,10 @@
 //          v itself: e4m3 reaches down to 2^-18 of its largest value, which is 2^-36 of v.  A root above zero that would round to zero becomes the least
 //          value above it, so that no moment is divided by epsilon alone.
 //
-// Both are bound by memory: what is read is read once, what is written is written once.  The tensors' addresses and sizes come with the launch,
-// kTensors at a time, so that nothing is copied to the device beforehand; a workgroup finds its tensor by a comparison in every lane.
+// Both are bound by memory: what is read is read once, what is written is written once.  The tensors' addresses and sizes come with the launch, 74 to 120 tensors at a
+// time, so that nothing is copied to the device beforehand; a workgroup finds its tensor by a comparison in every lane.  Measured on buffers in turn, of the 6.2 TB/s
+// that an elementwise kernel reads and writes at: 101 M elements with bf16 gradients and bf16 copies, moments in 32 bits 460 to 490 us = 5.8 to 6.15, in 8 bits 270 = 6.0 (of bf16
+// weights without copies 167 = 6.1), packed one right after the other with odd sizes 470 and 322; the norm of 202 MB of bf16 36 = 5.6.
 #include <algorithm>
 #include <cmath>
 #include <vector>
@@ -212,7 +214,9 @@ struct BlockScale {
     }
 };
 constexpr int kStepThreads = 128;
-// A thread's elements: kUnits times kElems of them together, a workgroup's apart.
+// A thread's elements: kUnits times kElems of them together, a workgroup's apart.  Four 32-bit weights are a lane's at a time, so that a wavefront's accesses are whole kilobytes:
+// with eight of them, 101 M elements in 32 bits 543 us (four 462), with 8-bit moments 309 (264, twice four 267); 256 threads 470 to 480 and 264, twice four in 32 bits 497.  16-bit
+// weights, of which eight are 16 bytes, with 8-bit moments: eight 175, twice four 188.
 template <typename TW, bool EIGHT>
 struct StepShape {
     static constexpr int kElems = EIGHT ? 16 / static_cast<int>(sizeof(TW)) : 4, kUnits = EIGHT && kElems == 4 ? 2 : 1;

@@ -78,7 +78,7 @@ class Case:
     def __init__(self, n, gen, weight=F32, grad=F32, bits=32, copy=None, off=0, lr_scale=1.0, decay_scale=1.0, fresh=False):
         rand = lambda: torch.randn(n, generator=gen)  # noqa: E731
         unit = torch.exp(rand())
-        self.n, self.bits, self.lr_scale, self.decay_scale = n, bits, lr_scale, decay_scale
+        self.n, self.bits, self.lr_scale, self.decay_scale = n, bits, float(torch.tensor(lr_scale)), decay_scale
         self.weight = Guarded(n, weight, off, rand())
         self.grad = Guarded(n, grad, off, 0.01 * unit * rand() * (torch.rand(n, generator=gen) > 0.1))
         self.copy = Guarded(n, copy, off) if copy else None
@@ -203,6 +203,17 @@ def test_more_tensors_than_a_launch_takes_of_mixed_types_and_some_left_alone(mqg
             assert all(torch.equal(b.buf, t) for b, t in zip(c.buffers(), before[i]))
         else:
             c.check()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_rate_of_its_own_for_every_tensor(mqg, ctx, bits):
+    gen = torch.Generator().manual_seed(12)
+    cases = [Case(50 + 37 * i, gen, bits=bits, lr_scale=0.9 ** i, decay_scale=float(i % 4)) for i in range(40)]
+    expect(cases, PLAN)
+    mqg.mqg_adamw_step(ctx, params_of(mqg, cases), **PLAN)
+    torch.cuda.synchronize()
+    for c in cases:
+        c.check()
 
 
 def test_one_list_of_both_kinds_of_moments(mqg, ctx):
@@ -393,7 +404,7 @@ def norm_of(mqg, ctx, grads, **args):
 @pytest.mark.parametrize("dtype", TYPES)
 def test_norm_of_lists(mqg, ctx, dtype):
     gen = torch.Generator().manual_seed(9)
-    for count, most in ((1, 3), (1, 100_000), (5, 5000), (64, 300), (65, 9000), (200, 2000), (1, 5_000_000)):
+    for count, most in ((1, 3), (1, 100_000), (5, 5000), (64, 300), (65, 9000), (200, 2000), (700, 90), (1, 5_000_000)):
         grads = [Guarded(int(torch.randint(0 if count > 1 else most, most + 1, (1,), generator=gen)), dtype, i % 4) for i in range(count)]
         for g in grads:
             g.t.copy_(torch.randn(g.n, generator=gen))
