@@ -205,6 +205,32 @@ def test_more_tensors_than_a_launch_takes_of_mixed_types_and_some_left_alone(mqg
             c.check()
 
 
+@pytest.mark.parametrize("grad", TYPES)
+def test_8_bit_moments_are_those_of_elementary_operations(mqg, ctx, grad):
+    """Bit for bit, step after step: products, sums, roots and quotients are each rounded to nearest in fp32, as torch's are one by one."""
+    n = 50_000
+    gen = torch.Generator().manual_seed(13)
+    weight = torch.randn(n, generator=gen).cuda()
+    params = mqg.Params([weight], [torch.zeros(n, dtype=grad, device="cuda")], state_dtype=E4M3)
+    unit = torch.exp(2 * torch.randn(n, generator=gen))
+    unit[:1000] = 0
+    m, v = torch.zeros(n, dtype=E4M3, device="cuda"), torch.zeros(n, dtype=E4M3, device="cuda")
+    ms, vs = torch.zeros(blocks_of(n), device="cuda"), torch.zeros(blocks_of(n), device="cuda")
+    scale = torch.full((1,), 0.37, device="cuda")
+    for step in range(1, 9):
+        g16 = (1e-3 * unit * torch.randn(n, generator=gen)).to(grad).cuda()
+        params.set_grads([g16])
+        mqg.mqg_adamw_step(ctx, params, grad_scale=scale, **dict(PLAN, step=step))
+        g = g16.float() * scale
+        m32 = 0.9 * (m.float() * spread_out(ms, n)) + (1 - 0.9) * g
+        root = (0.999 * (v.float() * spread_out(vs, n)).square() + (1 - 0.999) * g * g).sqrt()
+        (m, ms), (v, vs) = quantised(m32), quantised(root, 2.0 ** -9)
+        torch.cuda.synchronize()
+        assert torch.equal(params.m_scale[0], ms) and torch.equal(params.v_scale[0], vs), step
+        # (zeros of either sign are the same value)
+        assert torch.equal(params.m[0].float(), m.float()) and torch.equal(params.v[0].float(), v.float()), step
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_a_rate_of_its_own_for_every_tensor(mqg, ctx, bits):
     gen = torch.Generator().manual_seed(12)

@@ -231,6 +231,21 @@ def test_rows_of_any_size_and_mean(mqg, ctx, dim, dtype):
     assert bool(((gw.double().cpu() - want[2]).abs() <= (40 + 60 + 101) * U * want[3]).all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [6, 100, 1100])
+def test_weight_and_bias_alone(mqg, ctx, dim, dtype):
+    gen = torch.Generator().manual_seed(15)
+    x = torch.randn((70, dim), generator=gen).to(dtype).cuda()
+    w, b = (1 + 0.3 * torch.randn(dim, generator=gen)).cuda(), torch.randn(dim, generator=gen).cuda()
+    ones, zeros = torch.ones(dim, device="cuda"), torch.zeros(dim, device="cuda")
+    for some, full in (((w, None), (w, zeros)), ((None, b), (ones, b)), ((None, None), (ones, zeros))):
+        got, want = torch.zeros_like(x), torch.zeros_like(x)
+        mqg.mqg_layer_norm(ctx, x, *some, y=got, eps=EPS)
+        mqg.mqg_layer_norm(ctx, x, *full, y=want, eps=EPS)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
 def test_offsets_beyond_32_bits(mqg, ctx):
     stride, dim = (1 << 31) + 64, 100                              # elements between two rows
     buf = torch.zeros(stride + dim, dtype=torch.float16, device="cuda")
