@@ -7,7 +7,7 @@
 // norm's rows are.  The mean is taken first and the squares are those of the differences from it, so that rows whose mean is large against their
 // spread keep it; what the mean was off by (the differences' own mean, which the same exchange gives) is taken out of both.  So a row has two exchanges between lanes.
 // Measured on buffers in turn, of the 6.2 TB/s that an elementwise kernel reads and writes at: forward 295,000 x 256 fp16 into e4m3 86 us = 6.2, 109,000 x 602 fp32 175 = 6.0,
-// 8,192 x 8,192 bf16 92 = 5.8; backward 295,000 x 256 fp16 99 us = 6.1, 109,000 x 602 fp32 176 = 6.0, 8,192 x 8,192 bf16 103 to 108 = 5.0 to 5.2.  Of a million e4m3 values 0.8 to 1.4 are the
+// 8,192 x 8,192 bf16 92 = 5.8; backward 295,000 x 256 fp16 102 us = 5.9, 109,000 x 602 fp32 176 = 6.0, 8,192 x 8,192 bf16 103 to 108 = 5.0 to 5.2.  Of a million e4m3 values 0.8 to 1.4 are the
 // neighbour of the one that the formula has in 64 bits (1.5 to 2.7 in elementary fp32 operations), of int8 1.9 to 2.2 (2.5 to 3.3).
 #include <algorithm>
 
@@ -630,9 +630,14 @@ RowShape grad_shape(int dim, int vec, int64_t rows) {
     return sh.lanes == kWave && sh.nv * vec > 16 ? RowShape{256, 1} : sh;
 }
 // Workgroups of a backward at most, each of which leaves its share of the gradients: as many as are on the chip together for the longest rows (8,192 x 8,192
-// bf16: 256 103 us, 512 116), more for short ones (2 M x 16 bf16: 512 79, 1,024 63) and for those of four wavefronts (20,000 x 2,000: 80 and 73); in between
-// 295,000 x 256 fp16 512 98, 1,024 105; 109,000 x 602 fp32 176 and 184.
-int grad_parts(const RowShape &sh) { return sh.lanes <= 16 || sh.lanes == 256 ? 1024 : sh.lanes * sh.nv >= 1024 ? 256 : 512; }
+// bf16: 256 103 us, 512 116) and for those of a wavefront (109,000 x 602 fp32: 512 176, 768 203), more for shorter ones, whose waits want others to fill them (258,000 x 174 bf16 512 107, 768
+// 87, 1,024 80; 500,000 x 64 fp32 768 87, 1,024 91; 295,000 x 256 fp16 512 98, 768 102, 1,024 110; 2 M x 16 bf16 512 79, 768 73, 1,024 66), and for those of four
+// wavefronts (20,000 x 2,000: 512 80, 1,024 73).
+int grad_parts(const RowShape &sh) {
+    if (sh.lanes <= 8 || sh.lanes == 256) return 1024;
+    if (sh.lanes <= 32) return 768;
+    return sh.lanes * sh.nv >= 1024 ? 256 : 512;
+}
 
 constexpr int kJoinGrid = 32;         // workgroups whose shares the last of them adds
 
