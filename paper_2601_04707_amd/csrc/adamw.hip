@@ -9,8 +9,8 @@
 //
 // Both are bound by memory: what is read is read once, what is written is written once.  The tensors' addresses and sizes come with the launch, 74 to 120 tensors at a
 // time, so that nothing is copied to the device beforehand; a workgroup finds its tensor by a comparison in every lane.  Measured on buffers in turn, of the 6.2 TB/s
-// that an elementwise kernel reads and writes at: 101 M elements with bf16 gradients and bf16 copies, moments in 32 bits 460 to 490 us = 5.8 to 6.15, in 8 bits 270 = 6.0 (of bf16
-// weights without copies 167 = 6.1), packed one right after the other with odd sizes 470 and 322; the norm of 202 MB of bf16 36 = 5.6.
+// that an elementwise kernel reads and writes at: 101 M elements with bf16 gradients and bf16 copies, moments in 32 bits 460 to 490 us = 5.8 to 6.15, in 8 bits 260 = 6.3 (of bf16
+// weights without copies 167 = 6.1), packed one right after the other with odd sizes 470 and 308; the norm of 202 MB of bf16 36 = 5.6.
 #include <algorithm>
 #include <cmath>
 #include <vector>
@@ -214,13 +214,13 @@ struct BlockScale {
     }
 };
 constexpr int kStepThreads = 128;
-// A thread's elements: kUnits times kElems of them together, a workgroup's apart.  Four 32-bit weights are a lane's at a time, so that a wavefront's accesses are whole kilobytes:
-// with eight of them, 101 M elements in 32 bits 543 us (four 462), with 8-bit moments 309 (264, twice four 267); 256 threads 470 to 480 and 264, twice four in 32 bits 497.  16-bit
-// weights, of which eight are 16 bytes, with 8-bit moments: eight 175, twice four 188.
+// A thread's elements.  Four 32-bit weights, or eight of 16 bits, are 16 bytes, and a wavefront's accesses to them a whole kilobyte.  101 M elements with bf16 gradients and copies: moments in
+// 32 bits by fours 462 us, by eights 543, twice four 497; 8-bit ones by fours 259, twice four 270, by eights 309, with 64 and 256 threads 263 and 266; bf16 weights with 8-bit moments by
+// eights 167, by fours 192.
 template <typename TW, bool EIGHT>
 struct StepShape {
-    static constexpr int kElems = EIGHT ? 16 / static_cast<int>(sizeof(TW)) : 4, kUnits = EIGHT && kElems == 4 ? 2 : 1;
-    static constexpr int kGroup = kStepThreads * kElems * kUnits;
+    static constexpr int kElems = EIGHT ? 16 / static_cast<int>(sizeof(TW)) : 4;
+    static constexpr int kGroup = kStepThreads * kElems;
     static constexpr int kScaleLanes = MQG_ADAMW_BLOCK / kElems;      // that share a scale
     static_assert(kGroup % MQG_ADAMW_BLOCK == 0 && kScaleLanes <= kWave, "a workgroup has whole blocks, a wavefront their lanes");
 };
@@ -231,99 +231,91 @@ struct StepNumbers {
     int32_t copy_type;
 };
 // One workgroup's elements of a tensor.  FULL: all of them are there; a bound at every access would have each load waited for before the next one.  LINES: the 8-bit moments
-// begin at whole cache lines; where they don't, lines that two wavefronts share are read through the caches, once (100 M elements of odd tensors, one right after the other, 323 us
-// and 355 past them; where they do, 277 and 269).
+// begin at whole cache lines; where they don't, lines that two wavefronts share are read through the caches, once (twice four elements a thread: 101 M elements of odd tensors, one right after the
+// other, 323 us and 355 past them; where they do, 277 and 269).
 template <typename TW, typename TG, bool EIGHT, bool COPY, bool PAST, bool FULL, bool LINES>
-__device__ __forceinline__ void step_group(const StepNumbers &n, void *const (&of)[StepArgs<EIGHT, COPY>::kPointers], int64_t base, int64_t end) {
+__device__ __forceinline__ void step_group(const StepNumbers &n, void *const (&of)[StepArgs<EIGHT, COPY>::kPointers], int64_t i, int64_t end) {
     using Args = StepArgs<EIGHT, COPY>;
     using Shape = StepShape<TW, EIGHT>;
-    constexpr int E = Shape::kElems, U = Shape::kUnits;
+    constexpr int E = Shape::kElems;
     TW *weight = static_cast<TW *>(of[kWeight]);
     const TG *grad = static_cast<const TG *>(of[kGrad]);
-    typename Some<TW, E>::Whole w_raw[U];
-    typename Some<TG, E>::Whole g_raw[U];
-    typename Some<float, E>::Whole m_raw[U], v_raw[U];
-    typename Words<E / 4>::Whole m8[U], v8[U];
-    float ms[U], vs[U];
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-        const int64_t i = base + k * kStepThreads * E;
-        g_raw[k] = load_some<PAST, FULL, E>(grad, i, end);
-        if constexpr (EIGHT) {
-            m8[k] = load_8bit<PAST && LINES, FULL, E>(static_cast<const uint8_t *>(of[kM]), i, end);
-            v8[k] = load_8bit<PAST && LINES, FULL, E>(static_cast<const uint8_t *>(of[kV]), i, end);
-            ms[k] = FULL || i < end ? static_cast<const float *>(of[Args::kMScale])[i / MQG_ADAMW_BLOCK] : 0.f;
-            vs[k] = FULL || i < end ? static_cast<const float *>(of[Args::kVScale])[i / MQG_ADAMW_BLOCK] : 0.f;
-        } else {
-            m_raw[k] = load_some<PAST, FULL, E>(static_cast<const float *>(of[kM]), i, end);
-            v_raw[k] = load_some<PAST, FULL, E>(static_cast<const float *>(of[kV]), i, end);
-        }
-        w_raw[k] = load_some<PAST, FULL, E>(weight, i, end);
+    typename Some<TW, E>::Whole w_raw;
+    typename Some<TG, E>::Whole g_raw;
+    typename Some<float, E>::Whole m_raw, v_raw;
+    typename Words<E / 4>::Whole m8, v8;
+    float ms, vs;
+    g_raw = load_some<PAST, FULL, E>(grad, i, end);
+    if constexpr (EIGHT) {
+        m8 = load_8bit<PAST && LINES, FULL, E>(static_cast<const uint8_t *>(of[kM]), i, end);
+        v8 = load_8bit<PAST && LINES, FULL, E>(static_cast<const uint8_t *>(of[kV]), i, end);
+        ms = FULL || i < end ? static_cast<const float *>(of[Args::kMScale])[i / MQG_ADAMW_BLOCK] : 0.f;
+        vs = FULL || i < end ? static_cast<const float *>(of[Args::kVScale])[i / MQG_ADAMW_BLOCK] : 0.f;
+    } else {
+        m_raw = load_some<PAST, FULL, E>(static_cast<const float *>(of[kM]), i, end);
+        v_raw = load_some<PAST, FULL, E>(static_cast<const float *>(of[kV]), i, end);
+    }
+    w_raw = load_some<PAST, FULL, E>(weight, i, end);
+    float w[E], m[E], v[E], root[E];
+    uint32_t most_m = 0, most_v = 0, least_v = ~0u;
+    if constexpr (EIGHT) {
+        of_e4m3<E / 4>(m8, m);
+        of_e4m3<E / 4>(v8, v);
     }
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-        const int64_t i = base + k * kStepThreads * E;
-        float w[E], m[E], v[E], root[E];
-        uint32_t most_m = 0, most_v = 0, least_v = ~0u;
+    for (int j = 0; j < E; ++j) {
         if constexpr (EIGHT) {
-            of_e4m3<E / 4>(m8[k], m);
-            of_e4m3<E / 4>(v8[k], v);
-        }
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            if constexpr (EIGHT) {
-                m[j] *= ms[k];
-                v[j] *= vs[k];
-                v[j] *= v[j];
-            } else {
-                m[j] = m_raw[k][j];
-                v[j] = v_raw[k][j];
-            }
-            const float g = static_cast<float>(g_raw[k][j]) * n.by;
-            m[j] = apart_add(n.beta1 * m[j], n.new1 * g);
-            v[j] = apart_add(n.beta2 * v[j], n.new2 * g * g);
-            root[j] = root_of(v[j]);
-            most_m = max_u32(most_m, __float_as_uint(m[j]) & 0x7FFFFFFFu);
-            most_v = max_u32(most_v, __float_as_uint(v[j]));
-            least_v = min(least_v, __float_as_uint(v[j]) - 1);         // (zero is none)
-        }
-        if (ballot64(least_v < __float_as_uint(0x1p-100f) - 1 || most_v > __float_as_uint(0x1p+126f))) {
-#pragma unroll
-            for (int j = 0; j < E; ++j) root[j] = sqrtf(v[j]);
-        }
-        const float none = n.eps == 0.f ? 0.f : -1.f;                  // the divisor that changes nothing
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const float under = fmaf(root[j], n.root_by, n.eps);
-            // to one unit of its last place; no divisor but zero is below fp32's normal numbers
-            const float inv = under == none ? 0.f : __builtin_amdgcn_rcpf(under);
-            w[j] = fmaf(static_cast<float>(w_raw[k][j]), n.keep, -(n.size * m[j] * inv));
-        }
-        store_some<PAST, FULL>(weight, i, end, w);
-        if constexpr (COPY) {
-            void *copy = of[Args::kCopy];
-            if (n.copy_type == MQG_F16) store_some<PAST, FULL>(static_cast<F16 *>(copy), i, end, w);
-            else if (n.copy_type == MQG_BF16) store_some<PAST, FULL>(static_cast<BF16 *>(copy), i, end, w);
-            else store_some<PAST, FULL>(static_cast<float *>(copy), i, end, w);
-        }
-        if constexpr (EIGHT) {
-            const BlockScale sm(__uint_as_float(lanes_max(most_m, Shape::kScaleLanes)));
-            const BlockScale sv(sqrtf(__uint_as_float(lanes_max(most_v, Shape::kScaleLanes))));
-            if (threadIdx.x % Shape::kScaleLanes == 0 && (FULL || i < end)) {
-                static_cast<float *>(of[Args::kMScale])[i / MQG_ADAMW_BLOCK] = sm.scale;
-                static_cast<float *>(of[Args::kVScale])[i / MQG_ADAMW_BLOCK] = sv.scale;
-            }
-            float y[E];
-#pragma unroll
-            for (int j = 0; j < E; ++j) y[j] = sm.of(m[j]);
-            store_8bit<PAST, FULL>(static_cast<uint8_t *>(of[kM]), i, end, y);
-#pragma unroll
-            for (int j = 0; j < E; ++j) y[j] = fmaxf(sv.of(root[j]), fminf(root[j] * 0x1p+100f, 0x1p-9f));     // (roots are 2^-75 at least: 2^-9, or zero of zero)
-            store_8bit<PAST, FULL>(static_cast<uint8_t *>(of[kV]), i, end, y);
+            m[j] *= ms;
+            v[j] *= vs;
+            v[j] *= v[j];
         } else {
-            store_some<PAST, FULL>(static_cast<float *>(of[kM]), i, end, m);
-            store_some<PAST, FULL>(static_cast<float *>(of[kV]), i, end, v);
+            m[j] = m_raw[j];
+            v[j] = v_raw[j];
         }
+        const float g = static_cast<float>(g_raw[j]) * n.by;
+        m[j] = apart_add(n.beta1 * m[j], n.new1 * g);
+        v[j] = apart_add(n.beta2 * v[j], n.new2 * g * g);
+        root[j] = root_of(v[j]);
+        most_m = max_u32(most_m, __float_as_uint(m[j]) & 0x7FFFFFFFu);
+        most_v = max_u32(most_v, __float_as_uint(v[j]));
+        least_v = min(least_v, __float_as_uint(v[j]) - 1);         // (zero is none)
+    }
+    if (ballot64(least_v < __float_as_uint(0x1p-100f) - 1 || most_v > __float_as_uint(0x1p+126f))) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) root[j] = sqrtf(v[j]);
+    }
+    const float none = n.eps == 0.f ? 0.f : -1.f;                  // the divisor that changes nothing
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        const float under = fmaf(root[j], n.root_by, n.eps);
+        // to one unit of its last place; no divisor but zero is below fp32's normal numbers
+        const float inv = under == none ? 0.f : __builtin_amdgcn_rcpf(under);
+        w[j] = fmaf(static_cast<float>(w_raw[j]), n.keep, -(n.size * m[j] * inv));
+    }
+    store_some<PAST, FULL>(weight, i, end, w);
+    if constexpr (COPY) {
+        void *copy = of[Args::kCopy];
+        if (n.copy_type == MQG_F16) store_some<PAST, FULL>(static_cast<F16 *>(copy), i, end, w);
+        else if (n.copy_type == MQG_BF16) store_some<PAST, FULL>(static_cast<BF16 *>(copy), i, end, w);
+        else store_some<PAST, FULL>(static_cast<float *>(copy), i, end, w);
+    }
+    if constexpr (EIGHT) {
+        const BlockScale sm(__uint_as_float(lanes_max(most_m, Shape::kScaleLanes)));
+        const BlockScale sv(sqrtf(__uint_as_float(lanes_max(most_v, Shape::kScaleLanes))));
+        if (threadIdx.x % Shape::kScaleLanes == 0 && (FULL || i < end)) {
+            static_cast<float *>(of[Args::kMScale])[i / MQG_ADAMW_BLOCK] = sm.scale;
+            static_cast<float *>(of[Args::kVScale])[i / MQG_ADAMW_BLOCK] = sv.scale;
+        }
+        float y[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) y[j] = sm.of(m[j]);
+        store_8bit<PAST, FULL>(static_cast<uint8_t *>(of[kM]), i, end, y);
+#pragma unroll
+        for (int j = 0; j < E; ++j) y[j] = fmaxf(sv.of(root[j]), fminf(root[j] * 0x1p+100f, 0x1p-9f));     // (roots are 2^-75 at least: 2^-9, or zero of zero)
+        store_8bit<PAST, FULL>(static_cast<uint8_t *>(of[kV]), i, end, y);
+    } else {
+        store_some<PAST, FULL>(static_cast<float *>(of[kM]), i, end, m);
+        store_some<PAST, FULL>(static_cast<float *>(of[kV]), i, end, v);
     }
 }
 
