@@ -894,6 +894,18 @@ int mqg_adamw_step(mqg_ctx *ctx, const mqg_param *params, int32_t num_params, co
         auto state = [](const mqg_param &p) { return p.numel * (p.state_type == MQG_STATE_E4M3 ? 1 : 4); };
         auto scales = [](const mqg_param &p) { return mqg::ceil_div(p.numel, MQG_ADAMW_BLOCK) * 4; };
         using Range = std::pair<const void *, int64_t>;
+        for (int32_t i = 0; i < num_params; ++i) {         // one tensor's own buffers, its gradient among them
+            const mqg_param &p = params[i];
+            if (!p.grad || p.numel == 0) continue;
+            const Range own[] = {{p.weight, p.numel * bytes(p.weight_type)}, {p.m, state(p)}, {p.v, state(p)}, {p.copy, p.copy ? p.numel * bytes(p.copy_type) : 0},
+                                 {p.grad, p.numel * bytes(p.grad_type)}};
+            for (int a = 0; a < 5; ++a)
+                for (int b = 0; b < a; ++b) {
+                    const uintptr_t x = reinterpret_cast<uintptr_t>(own[a].first), y = reinterpret_cast<uintptr_t>(own[b].first);
+                    if (x && y && x < y + static_cast<uintptr_t>(own[b].second) && y < x + static_cast<uintptr_t>(own[a].second))
+                        return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: a tensor's weight, copy, moments or gradient share memory");
+                }
+        }
         if (overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.weight, p.numel * bytes(p.weight_type)); }) ||
             overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.copy, p.numel * bytes(p.copy_type)); }) ||
             overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.m, state(p)); }) ||

@@ -506,6 +506,9 @@ def test_refusals(mqg, ctx):
         assert step(lambda c: setattr(c[0], field, getattr(c[1], field) + 4 * 299)) == bad
     for field in ("m_scale", "v_scale"):
         assert step(lambda c: setattr(c[1], field, getattr(c[0], field)), bits=8) == bad
+    # one buffer in two places of the same tensor
+    for a, b in (("m", "v"), ("weight", "m"), ("v", "grad"), ("weight", "grad"), ("copy", "weight"), ("copy", "grad")):
+        assert step(lambda c: setattr(c[1], a, getattr(c[1], b))) == bad and b"share" in mqg.lib.mqg_last_error(ctx.h)
     # what has no gradient is not looked at
     assert step(lambda c: (setting("grad", None)(c), setting("weight", None)(c))) == mqg.MQG_OK
 
