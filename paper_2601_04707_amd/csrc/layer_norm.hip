@@ -229,8 +229,10 @@ struct Unit {
     float low, high;
 };
 __device__ __forceinline__ bool odd_row(float var, float eps, float c) { return odd_mean(var + eps) || c * c > var; }
-__device__ __forceinline__ Unit odd_unit(float mean) {
-    return mean < 0x1p-100f ? Unit{1.f, 0x1p+90f} : mean <= 0x1p+100f ? Unit{1.f, 1.f} : Unit{0x1p-80f, 1.f};
+// A mean that is off by c, far more than the row spreads, leaves nothing of the variance beside c^2: it may read zero where the row spreads up to 2^-8 c.  Such a row's values differ by
+// 2^-13 c or more (a last place of s; c is 2^-11 of the mean at most), and so it is by c that it is known to be none of the smallest: its squares would leave 32 bits' range times 2^180.
+__device__ __forceinline__ Unit odd_unit(float mean, float c) {
+    return mean < 0x1p-100f && c * c < 0x1p-66f ? Unit{1.f, 0x1p+90f} : mean <= 0x1p+100f ? Unit{1.f, 1.f} : Unit{0x1p-80f, 1.f};
 }
 // The variance of the row times unit, and eps, or infinity, whose factor is 0, where the row's own factor is above 32 bits' numbers: rows of equal values without an
 // epsilon, and such as spread less than 2^-128.
@@ -327,7 +329,7 @@ k_layer_norm(LayerArgs a) {
         if (!odd_row(var, a.eps, c)) {                     // (the same in all lanes of a row)
             r = reciprocal_root(var + a.eps);
         } else {
-            const Unit u = odd_unit(var + a.eps);
+            const Unit u = odd_unit(var + a.eps, c);
             const float s0 = lanes.first(s[0][0]) * u.low;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
@@ -522,7 +524,7 @@ k_layer_norm_backward(LayerGradArgs a) {
         if (!odd_row(var, a.eps, c)) {
             put_row(plain, reciprocal_root(var + a.eps), 1.f);
         } else {
-            const Unit u = odd_unit(var + a.eps);
+            const Unit u = odd_unit(var + a.eps, c);
             const float s0 = lanes.first(plain(0, 0)) * u.low;
             auto scaled = [&](int k, int j) __attribute__((always_inline)) {
                 const float d = (static_cast<float>(v.s[k][j]) * u.low - s0) * u.high;
