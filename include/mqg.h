@@ -710,7 +710,8 @@ int mqg_layer_norm(mqg_ctx *ctx, const void *x, int64_t x_stride, const void *re
                    int64_t scale_stride, mqg_stream stream);
 
 /*
- * Its backward.  With d and R = 1/sqrt(mean(d^2) + eps) of the forward's s, 0 where the forward gives the bias, u = d R and h = grad_y * weight:
+ * Its backward.  With d and R = 1/sqrt(mean(d^2) + eps) of the forward's s, 0 where that is above fp32's numbers (rows of equal values with eps = 0, and rows that spread
+ * less than 2^-128), u = d R and h = grad_y * weight:
  *   grad_x = R (h - mean(h) - u mean(h u)) + grad_sum   (the gradient of x and of residual)
  *   grad_weight[c] = sum over the rows of grad_y * u,  grad_bias[c] = sum over the rows of grad_y    (device float [dim], written;
  *                    NULL if not wanted)

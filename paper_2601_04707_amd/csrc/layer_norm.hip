@@ -497,9 +497,9 @@ k_layer_norm_backward(LayerGradArgs a) {
             if (kOpaque) { as_loaded(v.s); as_loaded(v.g); }
             dot = then[2] * a.per_dim - c * h_mean;
         };
-        // r: of the values times `unit`
-        auto put_row = [&](auto value, float r, float unit) __attribute__((always_inline)) {
-            const float by = r * unit, cr = c * r;
+        // r: that of the values that are taken; by: the row's own
+        auto put_row = [&](auto value, float r, float by) __attribute__((always_inline)) {
+            const float cr = c * r;
             dot *= r;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
@@ -522,7 +522,8 @@ k_layer_norm_backward(LayerGradArgs a) {
         auto plain = [&](int k, int j) __attribute__((always_inline)) { return static_cast<float>(v.s[k][j]); };
         stats(plain);
         if (!odd_row(var, a.eps, c)) {
-            put_row(plain, reciprocal_root(var + a.eps), 1.f);
+            const float r = reciprocal_root(var + a.eps);
+            put_row(plain, r, r);
         } else {
             const Unit u = odd_unit(var + a.eps, c);
             const float s0 = lanes.first(plain(0, 0)) * u.low;
@@ -531,7 +532,9 @@ k_layer_norm_backward(LayerGradArgs a) {
                 return (places.own[k] >> j) & 1 ? d : 0.f;
             };
             stats(scaled);
-            put_row(scaled, 1.0f / sqrtf(unit_variance(var, a.eps, u.low * u.high)), u.low * u.high);
+            const float unit = u.low * u.high, r = 1.0f / sqrtf(unit_variance(var, a.eps, unit));
+            // (of equal values so large that their sums leave 32 bits' range: their differences are zeros, whatever r is, but eps is below 32 bits' numbers times unit^2)
+            put_row(scaled, r, unit < 1.f && var == 0.f && a.eps > 0.f ? 1.0f / sqrtf(a.eps) : r * unit);
         }
         gx += step * a.gx_stride;
     }
