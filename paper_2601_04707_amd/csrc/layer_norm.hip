@@ -228,7 +228,8 @@ __device__ __forceinline__ float reciprocal_root(float v) {
 struct Unit {
     float low, high;
 };
-__device__ __forceinline__ bool odd_row(float var, float eps, float c) { return odd_mean(var + eps) || c * c > var; }
+// (c^2 and the variance of small values may both be below 32 bits' numbers, and read zero)
+__device__ __forceinline__ bool odd_row(float var, float eps, float c) { return odd_mean(var + eps) || (c * c >= var && c != 0.f); }
 // A mean that is off by c, far more than the row spreads, leaves nothing of the variance beside c^2: it may read zero where the row spreads up to 2^-8 c.  Such a row's values differ by
 // 2^-13 c or more (a last place of s; c is 2^-11 of the mean at most), and so it is by c that it is known to be none of the smallest: its squares would leave 32 bits' range times 2^180.
 __device__ __forceinline__ Unit odd_unit(float mean, float c) {

@@ -62,3 +62,24 @@ def test_the_gradient_goes_through_the_mean(mqg, ctx, dim, dtype):
         terms = factor * (h.abs() + h.abs().mean(1, keepdim=True)) + gs.double().cpu().abs()
         assert bool(((gx.double().cpu() - want).abs() <= 192 * U * terms + UNIT[dtype] * 1.0001 * want.abs() + LEAST[dtype]).all()), eps
         assert bool(((gb.double().cpu() - gy.double().cpu().sum(0)).abs() <= (rows + 60) * U * gy.double().cpu().abs().sum(0)).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", DIMS)
+def test_the_bias_and_nothing_else(mqg, ctx, dim, dtype):
+    gen = torch.Generator().manual_seed(dim)
+    x = rows_of(dim, dtype)
+    rows = x.shape[0]
+    gy = torch.randn((rows, dim), generator=gen).to(dtype).cuda()
+    w, b = (1 + 0.3 * torch.randn(dim, generator=gen)).cuda(), torch.randn(dim, generator=gen).cuda()
+    for eps in epsilons(dtype) + (0.0,):
+        y, z, gx = (torch.full_like(x, 3.0) for _ in range(3))
+        gw = torch.full((dim,), 3.0, device="cuda")
+        q, scale = torch.ones((rows, dim), dtype=torch.int8, device="cuda"), torch.zeros((rows, 1), device="cuda")
+        mqg.mqg_layer_norm(ctx, x, w, b, y=y, eps=eps)
+        mqg.mqg_layer_norm(ctx, x, w, None, y=z, q=q, q_scale=scale, eps=eps)
+        mqg.mqg_layer_norm_backward(ctx, gy, x, w, gx, grad_weight=gw, eps=eps)
+        torch.cuda.synchronize()
+        assert torch.equal(y, b.to(dtype).expand_as(y)), eps
+        assert bool((z == 0).all()) and bool((q == 0).all()) and bool((scale == 2.0 ** -126).all()), eps
+        assert bool((gw == 0).all()), eps
