@@ -383,7 +383,10 @@ constexpr int kJoinParts = kWave;                      // so many workgroups at 
 __device__ __forceinline__ void end_norm(const NormEnd &e, double squares) {
     const float found = static_cast<float>(e.mul * sqrt(squares));
     if (e.norm) *e.norm = found;
-    if (e.scale) *e.scale = found < __uint_as_float(0x7F800000u) ? e.mul * fminf(e.most * (1.0f / found), 1.f) : __uint_as_float(0x7FC00000u);
+    if (!e.scale) return;
+    // (the reciprocal of a norm below 2^-126 may be infinite, and that of one above 2^126 has lost bits)
+    const float share = found >= 0x1p-126f && found <= 0x1p+126f ? e.most * (1.0f / found) : e.most / found;
+    *e.scale = found < __uint_as_float(0x7F800000u) ? e.mul * fminf(share, 1.f) : __uint_as_float(0x7FC00000u);
 }
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
