@@ -780,7 +780,7 @@ typedef enum { MQG_STATE_F32 = 0, MQG_STATE_E4M3 = 1 } mqg_state_type;
 
 /*
  * A tensor that an optimiser steps: numel elements, one after the other.  What is written (weight, copy, m, v and their scales) overlaps
- * no other buffer of the call.  Any alignment of the element.
+ * no other buffer of the call (a step of tensors whose buffers do is refused); gradients may share memory with one another.  Any alignment of the element.
  */
 typedef struct mqg_param {
     int64_t numel;

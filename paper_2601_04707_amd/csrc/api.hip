@@ -4,10 +4,9 @@
 #include <cstdint>
 #include <cstring>
 #include <new>
-#include <utility>
-#include <vector>
 
 #include "common.h"
+#include "param_ranges.h"
 
 namespace {
 thread_local std::string g_create_error = "";
@@ -24,23 +23,6 @@ int guarded(F call) {
     } catch (...) {
         return MQG_ERR_HIP;
     }
-}
-
-// The written ranges of one kind of buffer in a list of parameters: two that overlap would be stepped by two workgroups at once.
-template <typename Of>
-bool overlapping(const mqg_param *params, int32_t num, Of of) {
-    std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
-    ranges.reserve(static_cast<size_t>(num));
-    for (int32_t i = 0; i < num; ++i)
-        if (params[i].grad && params[i].numel > 0) {
-            const std::pair<const void *, int64_t> r = of(params[i]);
-            const uintptr_t at = reinterpret_cast<uintptr_t>(r.first);
-            if (r.first) ranges.emplace_back(at, at + static_cast<uintptr_t>(r.second));
-        }
-    if (!std::is_sorted(ranges.begin(), ranges.end())) std::sort(ranges.begin(), ranges.end());
-    for (size_t i = 1; i < ranges.size(); ++i)
-        if (ranges[i].first < ranges[i - 1].second) return true;
-    return false;
 }
 
 template <typename T>
@@ -890,29 +872,8 @@ int mqg_adamw_step(mqg_ctx *ctx, const mqg_param *params, int32_t num_params, co
             if (!std::isfinite(p.lr_scale) || !std::isfinite(p.decay_scale))
                 return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: lr_scale or decay_scale is not finite");
         }
-        auto bytes = [](int32_t dtype) { return dtype == MQG_F32 ? 4 : 2; };
-        auto state = [](const mqg_param &p) { return p.numel * (p.state_type == MQG_STATE_E4M3 ? 1 : 4); };
-        auto scales = [](const mqg_param &p) { return mqg::ceil_div(p.numel, MQG_ADAMW_BLOCK) * 4; };
-        using Range = std::pair<const void *, int64_t>;
-        for (int32_t i = 0; i < num_params; ++i) {         // one tensor's own buffers, its gradient among them
-            const mqg_param &p = params[i];
-            if (!p.grad || p.numel == 0) continue;
-            const Range own[] = {{p.weight, p.numel * bytes(p.weight_type)}, {p.m, state(p)}, {p.v, state(p)}, {p.copy, p.copy ? p.numel * bytes(p.copy_type) : 0},
-                                 {p.grad, p.numel * bytes(p.grad_type)}};
-            for (int a = 0; a < 5; ++a)
-                for (int b = 0; b < a; ++b) {
-                    const uintptr_t x = reinterpret_cast<uintptr_t>(own[a].first), y = reinterpret_cast<uintptr_t>(own[b].first);
-                    if (x && y && x < y + static_cast<uintptr_t>(own[b].second) && y < x + static_cast<uintptr_t>(own[a].second))
-                        return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: a tensor's weight, copy, moments or gradient share memory");
-                }
-        }
-        if (overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.weight, p.numel * bytes(p.weight_type)); }) ||
-            overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.copy, p.numel * bytes(p.copy_type)); }) ||
-            overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.m, state(p)); }) ||
-            overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.v, state(p)); }) ||
-            overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.state_type == MQG_STATE_E4M3 ? p.m_scale : nullptr, scales(p)); }) ||
-            overlapping(params, num_params, [&](const mqg_param &p) { return Range(p.state_type == MQG_STATE_E4M3 ? p.v_scale : nullptr, scales(p)); }))
-            return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: two tensors share a weight, copy, moment or scale");
+        if (mqg::step_shares_memory(params, num_params, {{plan->step_dev, sizeof(int64_t)}, {plan->lr_dev, sizeof(float)}, {plan->grad_scale_dev, sizeof(float)}}))
+            return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_adamw_step: a weight, copy, moment or scale shares memory with another buffer of the call");
         return mqg::run_adamw_step(ctx, params, num_params, plan, static_cast<hipStream_t>(stream));
     });
 }
