@@ -771,6 +771,8 @@ class Params:
     def __init__(self, weights=None, grads=None, *, m=None, v=None, m_scale=None, v_scale=None, copies=None, state_dtype=torch.float32,
                  lr_scale=None, decay_scale=None):
         assert weights is not None or grads is not None
+        # lists of its own: the library has the addresses of these tensors, whatever the caller puts into its lists later
+        weights, m, v, m_scale, v_scale, copies = (None if given is None else list(given) for given in (weights, m, v, m_scale, v_scale, copies))
         like = weights if weights is not None else grads
         n = len(like)
         eight = (m[0].dtype if m else state_dtype) == torch.float8_e4m3fn
