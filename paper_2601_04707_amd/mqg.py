@@ -813,14 +813,17 @@ class Params:
 
     def set_grads(self, grads) -> None:
         """The gradients of the steps that follow."""
+        grads = list(grads)
         assert len(grads) == len(self.c)
-        for i, (p, g) in enumerate(zip(self.c, grads)):
+        like = self.weights if self.weights is not None else grads
+        # (looked at before anything is changed: `grads` keeps alive what the addresses are of)
+        new = [None if g is None else (self._data(g, like[i].shape), _layer_dtype(g), g.numel()) for i, g in enumerate(grads)]
+        for p, g in zip(self.c, new):
             if g is None:
                 p.grad = None
             else:
-                p.grad, p.grad_type = self._data(g, self.weights[i].shape if self.weights is not None else g.shape), _layer_dtype(g)
-                p.numel = g.numel()
-        self.grads = list(grads)
+                p.grad, p.grad_type, p.numel = g
+        self.grads = grads
 
 
 def _one(t, dtype) -> Optional[int]:

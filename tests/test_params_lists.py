@@ -40,3 +40,14 @@ def test_lists_that_the_caller_changes(mqg, eight):
     params.set_grads([None, torch.zeros(200), None])
     with pytest.raises(AssertionError):
         params.set_grads([None, torch.zeros(199), None])
+
+
+def test_gradients_that_are_refused_leave_those_before(mqg):
+    params = mqg.Params([torch.zeros(8) for _ in range(2)])
+    first = [torch.ones(8), torch.ones(8, dtype=torch.float16)]
+    params.set_grads(first)
+    for wrong in ([torch.ones(8, dtype=torch.bfloat16), torch.ones(7)], [None, torch.ones(8, dtype=torch.float64)], [torch.ones(8)]):
+        with pytest.raises((AssertionError, TypeError)):
+            params.set_grads(wrong)
+        assert [(p.grad, p.grad_type) for p in params.c] == [(first[0].data_ptr(), mqg.MQG_F32), (first[1].data_ptr(), mqg.MQG_F16)]
+        assert all(a is b for a, b in zip(params.grads, first))
