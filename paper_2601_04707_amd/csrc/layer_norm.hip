@@ -416,7 +416,7 @@ k_layer_norm_backward(LayerGradArgs a) {
     float w[NV][V];
 #pragma unroll
     for (int k = 0; k < NV; ++k) load_weight(a.weight, places.at[k], dim, w[k]);
-    constexpr bool kInLds = kThreads >= 1024 && NV >= 2;   // (rows of 16,384: 4,000 of bf16 243 -> 166 us, 2,000 of fp32 207 -> 155; in LDS rows of 8,192 bf16 116 -> 137)
+    constexpr bool kInLds = kThreads >= 1024 && NV >= 2;   // (rows of 16,384, with all loads through the caches: 4,000 of bf16 243 -> 166 us, 2,000 of fp32 207 -> 155; in LDS rows of 8,192 bf16 116 -> 137.  With loads past them 136 and 125)
     using Own = OwnSums<NV, V, kThreads, kInLds>;
     __shared__ typename Own::Quad own[2 * Own::kQuads];
     Own gw(own), gb(own + Own::kQuads);

@@ -8,7 +8,7 @@
 namespace mqg {
 namespace {
 
-constexpr int kNormParts = 512;      // workgroups of a backward at most
+constexpr int kNormParts = 512;      // workgroups of the root-mean-square norm's backward at most
 
 __device__ __forceinline__ int64_t rows_of(const int64_t *num_rows, int64_t cap) {
     if (!num_rows) return cap;

@@ -765,7 +765,7 @@ class Params:
 
     weights, grads: lists of contiguous tensors of the same shapes (a gradient of None: the tensor is left alone); without weights the list
     serves mqg_grad_norm only.  m, v: the moments, zeros of state_dtype if not given - float32, or float8_e4m3fn (v: its root) with
-    m_scale, v_scale, a float32 per MQG_ADAMW_BLOCK elements.  copies: tensors that receive the weights rounded to their type.
+    m_scale, v_scale, a float32 per MQG_ADAMW_BLOCK elements (both zeros if not given: moments of zero, whatever m and v hold).  copies: tensors that receive the weights rounded to their type.
     lr_scale, decay_scale: a number for every tensor."""
 
     def __init__(self, weights=None, grads=None, *, m=None, v=None, m_scale=None, v_scale=None, copies=None, state_dtype=torch.float32,
