@@ -646,7 +646,7 @@ int mqg_weighted_aggregate_backward(mqg_ctx *ctx, const mqg_block *block, const 
  * columns) and mqg_orthogonalize and mqg_muon_step (for stacks of num_mats matrices of rows x cols) would
  * otherwise allocate when they are first called at that size, after a synchronisation of their stream
  * (it synchronises the device itself where it replaces smaller scratch, and is not for a time at which a stream is recorded):
- * up to 8 KiB per column (the root-mean-square norm takes 2); 8 KiB per matrix, 12 bytes per element and 8 per element of the smaller side's square, sides rounded up to
+ * up to 8 KiB per column for up to 2,048 columns, and for more 16 MiB or 2 KiB per column, whichever is more (the root-mean-square norm alone takes 2 KiB per column); 8 KiB per matrix, 12 bytes per element and 8 per element of the smaller side's square, sides rounded up to
  * multiples of 64 or 128, but nothing for matrices that one workgroup holds (with n and k sides in units of 32, n <= k, rounded up: n k <= 16
  * and 2 n k + n^2 <= 39, up to 32 x 512, 64 x 256 and 96 x 160).
  * While a stream is recorded into a HIP graph nothing is allocated: a call that would have to is

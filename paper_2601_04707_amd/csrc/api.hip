@@ -884,7 +884,7 @@ int mqg_ctx_reserve_layer(mqg_ctx *ctx, int32_t norm_dim, int32_t num_mats, int3
         if (norm_dim < 0 || num_mats < 0 || rows < 0 || cols < 0) return fail(ctx, MQG_ERR_INVALID_ARG, "mqg_ctx_reserve_layer: negative size");
         if (norm_dim > MQG_NORM_MAX_DIM || num_mats > MQG_ORTH_MAX_MATS || rows > MQG_ORTH_MAX_SIDE || cols > MQG_ORTH_MAX_SIDE)
             return fail(ctx, MQG_ERR_UNSUPPORTED, "mqg_ctx_reserve_layer: above the calls' limits");
-        return mqg::reserve_layer_scratch(ctx, std::max(mqg::layer_norm_scratch_bytes(norm_dim), mqg::orth_scratch_bytes(num_mats, rows, cols)),
+        return mqg::reserve_layer_scratch(ctx, std::max({mqg::norm_scratch_bytes(norm_dim), mqg::layer_norm_scratch_bytes(norm_dim), mqg::orth_scratch_bytes(num_mats, rows, cols)}),
                                           "mqg_ctx_reserve_layer");
     });
 }

@@ -15,9 +15,6 @@
 
 namespace mqg {
 
-// (rows of 2,048 columns and less may have 1,024 workgroups, others have 512: grad_parts)
-int64_t layer_norm_scratch_bytes(int32_t dim) { return std::max(std::min<int64_t>(dim, 2048) * 1024, int64_t(dim) * 512) * 2 * int64_t(sizeof(float)); }
-
 namespace {
 
 // A call that moves more than the chip's memory-side cache holds goes past the caches, with its loads, too (buffers that it doesn't hold from the call before: 295,000 x 256 fp16
@@ -645,6 +642,22 @@ int grad_parts(const RowShape &sh) {
     return sh.lanes * sh.nv >= 1024 ? 256 : 512;
 }
 
+}  // namespace
+
+// The shares of both gradients of rows of up to dim columns, of any type and number: a layout's widest rows have the most (few rows have a workgroup each at most).
+int64_t layer_norm_scratch_bytes(int32_t dim) {
+    int64_t floats = 2 * int64_t(kFewRows) * dim;
+    for (int vec : {4, 8})
+        for (int vecs : {4, 8, 16, 32, 64, 128, 192, 256, 512, 1024, 2048, 4096}) {
+            const int widest = std::min(vecs * vec, dim);
+            floats = std::max(floats, 2 * int64_t(widest) * grad_parts(grad_shape(widest, vec, INT64_MAX)));
+            if (widest == dim) break;
+        }
+    return floats * int64_t(sizeof(float));
+}
+
+namespace {
+
 constexpr int kJoinGrid = 32;         // workgroups whose shares the last of them adds
 
 #define MQG_GRAD_SHAPES(T, GO)                                     \
@@ -688,7 +701,7 @@ int launch_layer_norm_backward(mqg_ctx *ctx, LayerGradArgs a, float *grad_weight
         a.weight_parts = grad_weight;
         a.bias_parts = grad_bias;
     } else if (wanted) {
-        int rc = ensure_layer_scratch(ctx, layer_norm_scratch_bytes(a.dim), s, "mqg_layer_norm_backward");
+        int rc = ensure_layer_scratch(ctx, std::max(layer_norm_scratch_bytes(a.dim), grid * a.pitch * int64_t(sizeof(float))), s, "mqg_layer_norm_backward");
         if (rc != MQG_OK) return rc;
         parts = reinterpret_cast<float *>(ctx->layer_scratch.data);
         a.weight_parts = grad_weight ? parts : nullptr;
